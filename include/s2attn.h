@@ -61,10 +61,11 @@ enum {
   S2ATTN_ERR_TOO_LARGE = -12,  /* tensor too large for the index arithmetic, or over a fixed limit */
   S2ATTN_ERR_STRIDE = -13,     /* a stride is negative, misaligned or smaller than the extent it spans */
   S2ATTN_ERR_SCRATCH = -14,    /* s2attn_bwd_ex_static: the problem needs more than S2ATTN_STATIC_SCRATCH_BYTES */
-  S2ATTN_ERR_ALGO = -15        /* S2ATTN_BWD_STORED_DS asked for a shape it does not cover */
+  S2ATTN_ERR_ALGO = -15,       /* S2ATTN_BWD_STORED_DS asked for a shape it does not cover */
+  S2ATTN_ERR_WINDOW = -16      /* window, sinks or max_kv outside its range */
 };
 
-enum { S2ATTN_BF16 = 0, S2ATTN_F32 = 1 };
+enum { S2ATTN_BF16 = 0, S2ATTN_F32 = 1, S2ATTN_E4M3 = 2 /* paged cache only */ };
 
 /* Which query heads use the shifted partition (Section 3.2; the attention-pattern
  * ablation of Section 4.3 uses the other two). */
@@ -202,6 +203,88 @@ S2ATTN_API int s2attn_bwd_ex_static(const s2attn_params* p, void* stream);
  * launch: after both), [3] after the dQ kernel
  * (and the partial-sum pass, when present).  Same semantics and errors otherwise. */
 S2ATTN_API int s2attn_bwd_ex_marked(const s2attn_params* p, void* stream, void* const* events);
+
+/* ---- Attention with a sliding window and sinks (contiguous tensors) ----------------------------------------------
+ * Plain causal attention in which query i sees key j iff j <= i and (i - j < window or j < sinks): the last `window`
+ * tokens, its own among them, and the first `sinks` tokens, which stay visible.  Forward and gradient.
+ * The parameter block is that of s2attn_fwd_ex / s2attn_bwd_ex: q, k, v, o, lse, dout, dq, dk, dv, workspace, B, N, H, Hkv,
+ * D, dtype, scale and the strides.  G, shift, shift_rule, wrap_variant, heads_total, head_offset and bwd_algo are not read:
+ * there are no groups and no head shifts, N may be any positive number and H may be odd.
+ * window >= 1; window >= N is plain causal attention.  sinks >= 0.  S2ATTN_ERR_WINDOW otherwise.
+ * A batch padded on the right needs nothing: no token sees a later one, and padding rows with dout = 0 leave
+ * the gradients of the others alone (k, v, dout of padding rows have to be finite). */
+S2ATTN_API int s2attn_check_window_args(const s2attn_params* p, int window, int sinks, int backward);
+/* Bytes of device workspace the backward wants; 0 if the shape fields are invalid.  It runs with less, down to the row terms
+ * (bf16) and the partial dk, dv of the sinks. */
+S2ATTN_API size_t s2attn_window_workspace_bytes(const s2attn_params* p, int window, int sinks);
+S2ATTN_API int s2attn_window_fwd(const s2attn_params* p, int window, int sinks, void* stream);
+S2ATTN_API int s2attn_window_bwd(const s2attn_params* p, int window, int sinks, void* stream);
+
+/* ---- A paged cache of keys and values, and attention over it ------------------------------------------------------
+ * The cache is `pages` pages of page_size tokens, (pages, page_size, Hkv, D) of k and of v.  Sequence b has kv_len[b]
+ * cached tokens; its token at position j lies in page page_table[b][j / page_size], place j % page_size.
+ * A call works on T packed rows (new tokens, the rows of all sequences one after the other): rows row_start[b] ...
+ * row_start[b + 1] - 1 are the LAST positions of sequence b, so row row_start[b + 1] - 1 is position kv_len[b] - 1 and
+ * kv_len counts the tokens of the call.  The same plan serves all three calls of a step:
+ *   s2attn_cache_write   puts k, v of the rows into the cache
+ *   s2attn_paged_fwd     attention of q of the rows over the cache: position p sees key j iff j <= p and (window == 0 or
+ *                        p - j < window or j < sinks)
+ *   s2attn_cache_read    k, v of the rows back (row_start of whole sequences reads all of them)
+ * row_start, kv_len and page_table live on the device and are not checked on the host; the kernels keep every access inside
+ * the tensors whatever they hold:
+ *   - a sequence may have no rows, and no cached tokens;
+ *   - rows that belong to no sequence (before row_start[0], from row_start[B] on) are left as they are;
+ *   - positions from table_cols * page_size on and pages outside [0, pages) do not exist: nothing is written there, they are read
+ *     as zeros, and their keys are invisible.  Memory of a page behind kv_len is never read: it may hold anything;
+ *   - a row that sees no key gets o = 0 and lse = -infinity (also where a sequence has more rows than cached tokens: rows at
+ *     negative positions are not written to the cache, are read as zeros and see nothing).
+ * Sequences may share pages (a common prefix).  Two rows of one s2attn_cache_write must not name the same place: which of
+ * them its bytes come from is undefined then.
+ *
+ * Types: rows bf16 or fp32; the cache in the rows' type, or S2ATTN_E4M3: OCP e4m3 values with one scale 2^(exp - 127)
+ * a (token, kv head) and tensor, exp in k_exp / v_exp (pages, page_size, Hkv).  The scale is the least power of two that
+ * brings the row's largest finite magnitude to 448 or less, between 2^-110 and 2^120; infinities and NaN are stored as NaN. */
+typedef struct s2attn_paged_params {
+  const void* q;          /* paged_fwd: (T, H, D) */
+  void* o;                /* paged_fwd: (T, H, D), contiguous */
+  float* lse;             /* paged_fwd: (H, T), natural log of the sum of exp of the visible scores; may be NULL */
+  void* k;                /* cache_write: in, cache_read: out; (T, Hkv, D) */
+  void* v;
+  void* k_cache;          /* (pages, page_size, Hkv, D) */
+  void* v_cache;
+  unsigned char* k_exp;   /* S2ATTN_E4M3: (pages, page_size, Hkv) */
+  unsigned char* v_exp;
+  const int* page_table;  /* (B, table_cols), rows table_stride apart */
+  const int* row_start;   /* (B + 1) */
+  const int* kv_len;      /* (B) */
+  void* workspace;        /* paged_fwd: partial outputs; may be NULL (see s2attn_paged_workspace_bytes) */
+  size_t workspace_bytes;
+  int T, B, H, Hkv, D;    /* D is 64 or 128; T may be 0.  cache_write and cache_read do not read H */
+  int pages, page_size, table_cols;
+  int dtype;              /* S2ATTN_BF16 or S2ATTN_F32: q, o, k, v */
+  int cache_dtype;        /* dtype, or S2ATTN_E4M3 */
+  int window, sinks;      /* paged_fwd; window 0: every earlier key is visible */
+  int max_kv;             /* the most cached tokens of a sequence, as far as the caller knows; 0: table_cols * page_size.  Only
+                             decides how finely the keys are dealt out: a number that is off costs time and nothing else */
+  float scale;            /* softmax scale; <= 0 means 1/sqrt(D) */
+  /* Element strides; all zero = contiguous.  The last axis is contiguous.  Multiples of 16 bytes, but those of the exponents,
+   * which may be any. */
+  long long q_strides[2], k_strides[2], v_strides[2];       /* {token, head} */
+  long long k_cache_strides[3], v_cache_strides[3];         /* {page, token, head} */
+  long long k_exp_strides[3], v_exp_strides[3];
+  long long table_stride;                                   /* 0: table_cols */
+} s2attn_paged_params;
+
+enum { S2ATTN_PAGED_WRITE = 0, S2ATTN_PAGED_READ = 1, S2ATTN_PAGED_FWD = 2 };
+
+/* Pure host check of a parameter block for one of the three calls. */
+S2ATTN_API int s2attn_check_paged_args(const s2attn_paged_params* p, int call);
+/* Bytes of device workspace s2attn_paged_fwd wants: fp32 partial outputs of pieces of the keys, for batches whose rows alone
+ * would leave the chip idle.  It runs with less, or none, in fewer pieces.  0 if the shape fields are invalid. */
+S2ATTN_API size_t s2attn_paged_workspace_bytes(const s2attn_paged_params* p);
+S2ATTN_API int s2attn_cache_write(const s2attn_paged_params* p, void* stream);
+S2ATTN_API int s2attn_cache_read(const s2attn_paged_params* p, void* stream);
+S2ATTN_API int s2attn_paged_fwd(const s2attn_paged_params* p, void* stream);
 
 /* Static, never-freed message for a return code. */
 S2ATTN_API const char* s2attn_strerror(int code);

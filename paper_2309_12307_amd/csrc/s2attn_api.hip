@@ -12,7 +12,29 @@
 #include "s2attn_device.h"
 #include "s2attn_launch.h"
 
+namespace s2 {
+
+// The kernels use gfx950-only instructions; refuse any other device.  The answer
+// per device ordinal is cached (0 unknown, 1 yes, 2 no).
+int check_device() {
+  static std::atomic<int> cache[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return S2ATTN_ERR_DEVICE;
+  int state = (dev >= 0 && dev < 64) ? cache[dev].load(std::memory_order_relaxed) : 0;
+  if (state == 0) {
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return S2ATTN_ERR_DEVICE;
+    state = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : 2;
+    if (dev >= 0 && dev < 64) cache[dev].store(state, std::memory_order_relaxed);
+  }
+  return state == 1 ? S2ATTN_OK : S2ATTN_ERR_DEVICE;
+}
+
+}  // namespace s2
+
 namespace {
+
+using s2::check_device;
 
 constexpr size_t kAlign = 256;
 
@@ -212,6 +234,86 @@ bool dq_reuses_input(const s2attn_params* p) {
   return meets(p->q, span_bytes(p->q_strides, p->B, p->N, p->H, p->D, elem)) || meets(p->o, n_o) || meets(p->dout, n_o);
 }
 
+// ---- window attention: one causal run of all tokens, no groups or shifts.
+struct WindowPlan {
+  int parts;
+  s2::Win win;
+  size_t rows, partial, far;   // bytes of the workspace: row terms, partial dk, dv of the parts, of the cut key tiles
+};
+
+constexpr int kMostSegments = 15, kMostCutTiles = 8;
+
+// The first keys' dK/dV is cut where the sinks are few key tiles and their queries more than their windows': a
+// segment then is as long as the other workgroups' chains, or more where that would take over kMostSegments.  With more sink
+// tiles their workgroups take all queries, as in plain causal attention.
+// The query heads of a kv head go in parts until there are two workgroups to a CU, in parts of 1024 query rows (fp32: 256) or more.
+WindowPlan window_plan(const s2attn_params* p, int window, int sinks, size_t avail) {
+  WindowPlan x;
+  std::memset(&x, 0, sizeof(x));
+  const bool f32 = p->dtype == S2ATTN_F32;
+  const int KT = f32 ? 64 : 128, QT = f32 ? 32 : 64, r = p->H / p->Hkv;
+  x.win.window = std::min(window, p->N);
+  x.win.sinks = std::min(sinks, p->N);
+  const int tiles = (x.win.sinks + KT - 1) / KT, all = (p->N + QT - 1) / QT;
+  const int main_tiles = std::min<long long>(all, (KT - 1LL + x.win.window + QT - 1) / QT);
+  if (tiles > 0 && tiles <= kMostCutTiles && all > main_tiles) {
+    x.win.sink_tiles = tiles;
+    x.win.seg_tiles = std::max(main_tiles, (all - main_tiles + kMostSegments - 1) / kMostSegments);
+    x.win.n_seg = (all - main_tiles + x.win.seg_tiles - 1) / x.win.seg_tiles;
+  }
+  x.rows = 2 * delta_bytes(p->B, p->N, p->H);
+  auto far = [&](int parts) {
+    return round_up((size_t)2 * parts * (1 + x.win.n_seg) * p->B * p->Hkv * x.win.sink_tiles * KT * p->D * sizeof(float), kAlign);
+  };
+  const long long blocks = (long long)p->B * p->Hkv * ((p->N + KT - 1) / KT);
+  const long long chain = (long long)r * std::min<long long>(p->N, (long long)x.win.window + KT);
+  x.parts = 1;
+  for (int n = 2; n <= r && blocks * x.parts < 512; ++n)
+    if (r % n == 0 && chain / n >= (f32 ? 256 : 1024) && x.rows + partial_bytes(p->B, p->N, p->Hkv, p->D, n) + far(n) <= avail)
+      x.parts = n;
+  x.partial = partial_bytes(p->B, p->N, p->Hkv, p->D, x.parts);
+  x.far = far(x.parts);
+  x.win.by_far = s2::div_by(std::max(1, x.win.sink_tiles * x.win.n_seg));
+  x.win.by_seg = s2::div_by(std::max(1, x.win.n_seg));
+  return x;
+}
+
+bool window_shape_valid(const s2attn_params* p) {
+  return p->B > 0 && p->N > 0 && p->H > 0 && p->Hkv > 0 && p->D > 0 && p->H % p->Hkv == 0;
+}
+
+// The block as one of a layer without groups: the checks and kernel arguments of window attention go by it.
+s2attn_params window_params(const s2attn_params* p) {
+  s2attn_params x = *p;
+  x.G = p->N;
+  x.shift = 0;
+  x.shift_rule = S2ATTN_SHIFT_NONE;
+  x.wrap_variant = S2ATTN_WRAP_JOINT;
+  x.heads_total = x.head_offset = 0;
+  x.bwd_algo = S2ATTN_BWD_RECOMPUTE;
+  return x;
+}
+
+int check_tensors(const s2attn_params* p, int backward);
+
+int check_window(const s2attn_params* p, int window, int sinks, int backward) {
+  if (!p) return S2ATTN_ERR_NULL;
+  if (p->dtype != S2ATTN_BF16 && p->dtype != S2ATTN_F32) return S2ATTN_ERR_DTYPE;
+  if (p->B <= 0 || p->N <= 0 || p->H <= 0 || p->Hkv <= 0 || p->D <= 0) return S2ATTN_ERR_DIM;
+  if (p->H % p->Hkv != 0) return S2ATTN_ERR_HEADS;
+  if (p->D != 64 && p->D != 128) return S2ATTN_ERR_HEADDIM;
+  if (window < 1 || sinks < 0) return S2ATTN_ERR_WINDOW;
+  // the limits of the kernels on groups, here with one group; key positions and window ends are non-negative ints
+  if ((long long)p->B * p->H * 2 > 65535 || p->N > (1 << 30)) return S2ATTN_ERR_TOO_LARGE;
+  if ((2.0 + kMostSegments) * p->B * p->H * (p->N / 64 + 2) > 2.0e9) return S2ATTN_ERR_TOO_LARGE;
+  const int rc = check_tensors(p, backward);
+  if (rc != S2ATTN_OK || !backward) return rc;
+  const WindowPlan x = window_plan(p, window, sinks, 0);
+  if (!p->workspace || p->workspace_bytes < x.rows + x.far) return S2ATTN_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(p->workspace) & (kAlign - 1)) != 0) return S2ATTN_ERR_ALIGN;
+  return S2ATTN_OK;
+}
+
 int check_common(const s2attn_params* p, int backward) {
   if (!p) return S2ATTN_ERR_NULL;
   if (p->dtype != S2ATTN_BF16 && p->dtype != S2ATTN_F32) return S2ATTN_ERR_DTYPE;
@@ -236,7 +338,24 @@ int check_common(const s2attn_params* p, int backward) {
   if ((long long)p->B * p->H * 2 > 65535 || (long long)p->N / p->G > 65535) return S2ATTN_ERR_TOO_LARGE;
   if (2.0 * p->B * p->H * (p->N / p->G) * (p->G / 64 + 2) > 2.0e9) return S2ATTN_ERR_TOO_LARGE;
   if ((double)p->B * p->N * p->H * p->D > 9.0e18 / 4) return S2ATTN_ERR_TOO_LARGE;
+  const int rc = check_tensors(p, backward);
+  if (rc != S2ATTN_OK) return rc;
+  if (backward) {
+    const int from = shifted_from(p, shift);
+    const bool mixed = kv_heads_mixed(p->H, p->Hkv, from);
+    const size_t need = workspace_bytes_least(p->B, p->N, p->H, p->Hkv, p->D, mixed);
+    if (!p->workspace || p->workspace_bytes < need) return S2ATTN_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(p->workspace) & (kAlign - 1)) != 0) return S2ATTN_ERR_ALIGN;
+    if (p->bwd_algo == S2ATTN_BWD_STORED_DS) {
+      if (!stored_ds_applies(p, shift, from)) return S2ATTN_ERR_ALGO;
+      if (ds_heads_per_pass(p, p->workspace_bytes - need) == 0) return S2ATTN_ERR_WORKSPACE;
+    }
+  }
+  return S2ATTN_OK;
+}
 
+// Strides and addresses of the tensors.
+int check_tensors(const s2attn_params* p, int backward) {
   const int align = p->dtype == S2ATTN_F32 ? 4 : 8;
   if (!strides_ok(p->q_strides, p->B, p->H, p->D, align) || !strides_ok(p->k_strides, p->B, p->Hkv, p->D, align) ||
       !strides_ok(p->v_strides, p->B, p->Hkv, p->D, align))
@@ -260,33 +379,8 @@ int check_common(const s2attn_params* p, int backward) {
       if (!x) return S2ATTN_ERR_NULL;
       if (!aligned16(x)) return S2ATTN_ERR_ALIGN;
     }
-    const int from = shifted_from(p, shift);
-    const bool mixed = kv_heads_mixed(p->H, p->Hkv, from);
-    const size_t need = workspace_bytes_least(p->B, p->N, p->H, p->Hkv, p->D, mixed);
-    if (!p->workspace || p->workspace_bytes < need) return S2ATTN_ERR_WORKSPACE;
-    if ((reinterpret_cast<uintptr_t>(p->workspace) & (kAlign - 1)) != 0) return S2ATTN_ERR_ALIGN;
-    if (p->bwd_algo == S2ATTN_BWD_STORED_DS) {
-      if (!stored_ds_applies(p, shift, from)) return S2ATTN_ERR_ALGO;
-      if (ds_heads_per_pass(p, p->workspace_bytes - need) == 0) return S2ATTN_ERR_WORKSPACE;
-    }
   }
   return S2ATTN_OK;
-}
-
-// The kernels use gfx950-only instructions; refuse any other device.  The answer
-// per device ordinal is cached (0 unknown, 1 yes, 2 no).
-int check_device() {
-  static std::atomic<int> cache[64];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return S2ATTN_ERR_DEVICE;
-  int state = (dev >= 0 && dev < 64) ? cache[dev].load(std::memory_order_relaxed) : 0;
-  if (state == 0) {
-    hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return S2ATTN_ERR_DEVICE;
-    state = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : 2;
-    if (dev >= 0 && dev < 64) cache[dev].store(state, std::memory_order_relaxed);
-  }
-  return state == 1 ? S2ATTN_OK : S2ATTN_ERR_DEVICE;
 }
 
 // Strides of a tensor with `heads` heads: the caller's, or contiguous (B, N, heads, D) when all zero.
@@ -443,6 +537,57 @@ static int run_bwd(const s2attn_params* p, void* stream, void* const* events) {
 
 int s2attn_bwd_ex(const s2attn_params* p, void* stream) { return run_bwd(p, stream, nullptr); }
 
+int s2attn_check_window_args(const s2attn_params* p, int window, int sinks, int backward) {
+  return check_window(p, window, sinks, backward);
+}
+
+size_t s2attn_window_workspace_bytes(const s2attn_params* p, int window, int sinks) {
+  if (!p || !window_shape_valid(p) || window < 1 || sinks < 0) return 0;
+  const WindowPlan x = window_plan(p, window, sinks, SIZE_MAX);
+  return x.rows + x.partial + x.far;
+}
+
+int s2attn_window_fwd(const s2attn_params* p, int window, int sinks, void* stream) {
+  int rc = check_window(p, window, sinks, 0);
+  if (rc == S2ATTN_OK) rc = check_device();
+  if (rc != S2ATTN_OK) return rc;
+  const s2attn_params local = window_params(p);
+  const WindowPlan x = window_plan(p, window, sinks, 0);
+  s2::KArgs a = make_kargs(&local);
+  a.ragged = 1;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  rc = p->dtype == S2ATTN_F32 ? s2::launch_window_fwd_f32(a, x.win, st) : s2::launch_window_fwd_bf16(a, x.win, st);
+  return rc == 0 ? S2ATTN_OK : S2ATTN_ERR_LAUNCH;
+}
+
+int s2attn_window_bwd(const s2attn_params* p, int window, int sinks, void* stream) {
+  int rc = check_window(p, window, sinks, 1);
+  if (rc == S2ATTN_OK) rc = check_device();
+  if (rc != S2ATTN_OK) return rc;
+  const s2attn_params local = window_params(p);
+  WindowPlan x = window_plan(p, window, sinks, p->workspace_bytes);
+  s2::KArgs a = make_kargs(&local);
+  a.ragged = 1;
+  char* ws = static_cast<char*>(p->workspace);
+  a.neg_delta = reinterpret_cast<float*>(ws);
+  a.lse2 = reinterpret_cast<float*>(ws + delta_bytes(p->B, p->N, p->H));
+  a.parts = x.parts;
+  a.by_parts = s2::div_by(a.parts);
+  if (a.parts > 1) a.dkv_partial = reinterpret_cast<float*>(ws + x.rows);
+  x.win.partial = reinterpret_cast<float*>(ws + x.rows + x.partial);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (p->dtype == S2ATTN_F32) {
+    rc = s2::launch_window_bwd_f32(a, x.win, st);
+  } else {
+    rc = s2::launch_delta_bf16(a, st);
+    if (rc == 0) rc = s2::launch_window_bwd_bf16(a, x.win, st);
+  }
+  // (the parts' sum leaves cut key tiles to the sum of their segments, which comes after it)
+  if (rc == 0 && a.parts > 1) rc = s2::launch_combine_partials(a, p->dtype, st);
+  if (rc == 0 && x.win.sink_tiles > 0) rc = s2::launch_sink_combine(a, x.win, p->dtype, st);
+  return rc == 0 ? S2ATTN_OK : S2ATTN_ERR_LAUNCH;
+}
+
 // ---- backward without a caller workspace: the row terms (and, for a kv head that serves both
 // head classes, the fp32 partial sums) live in a device array that is part of the library's
 // code object.  Every GPU the library runs on holds its own copy at its own address, so the
@@ -544,6 +689,7 @@ const char* s2attn_strerror(int code) {
     case S2ATTN_ERR_STRIDE: return "a stride is negative, misaligned or smaller than the extent it spans";
     case S2ATTN_ERR_ALGO: return "S2ATTN_BWD_STORED_DS needs bf16, G a multiple of 128, shift (and a Variant 2 split) of 64 (128), and no kv head serving both head classes";
     case S2ATTN_ERR_SCRATCH: return "the backward needs more scratch than the library's static 16 MiB: call s2attn_bwd_ex with a workspace";
+    case S2ATTN_ERR_WINDOW: return "need window >= 1 (paged: >= 0), sinks >= 0 and max_kv >= 0";
     default: return "unknown s2attn error code";
   }
 }

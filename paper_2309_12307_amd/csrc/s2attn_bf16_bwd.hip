@@ -115,16 +115,22 @@ __device__ __forceinline__ void loop_phase() { asm volatile(".p2align 3"); }
 // path.  N = 100000, H = 32, G = 25000: forward + backward 86.9 ms with a dK/dV kernel of its own for
 // these shapes (one wave per SIMD, every row staged by itself) and the four-wave forward, 82.1 ms
 // with this one and the eight-wave forward.
-template <bool SPILL, bool RAGGED>
-__device__ __forceinline__ void dkdv_workgroup(const KArgs& a, int T, const Deal& deal, int block, int tid, char* smem) {
+// WINDOW (with RAGGED): one run of all tokens, the query tiles that meet the keys' windows (query_tiles).
+template <bool SPILL, bool RAGGED, bool WINDOW = false>
+__device__ __forceinline__ void dkdv_workgroup(const KArgs& a, int T, const Deal& deal, int block, int tid, char* smem,
+                                               const Win& win = Win{}) {
   const int lane = tid & 63, w = uni(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
   const bool role_b = w >= 4;
   const int kb = w & 3;
 
   // block -> (batch, kv head, part of its query heads, group, key tile); heaviest key tiles (jt = 0) first
-  int seq, jt;
-  if (!decode_block(block, T, deal, seq, jt)) return;
+  int seq, jt, segment = 0;
+  if constexpr (WINDOW) {
+    if (!decode_window(win, block, T, deal, seq, jt, segment)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, jt)) return;
+  }
   const KvPos at = kv_of_seq(a, seq);
   const int gidx = at.g, c = at.c, b = at.b;
   int h_lo, nheads, s;                               // query heads [h_lo, h_lo + nheads), all of one class
@@ -142,8 +148,15 @@ __device__ __forceinline__ void dkdv_workgroup(const KArgs& a, int T, const Deal
   const int key = kw0 + l32;
   const int split = uni(split_of_group(a, gidx, s));
   const int q_end = RAGGED ? run.len : (j0 < split ? split : a.G);
-  const int nq = uni((q_end - j0 + kQT - 1) / kQT);   // query tiles of one head
-  const int n_iter = nheads * nq;
+  int it_last = 0;                                    // query tiles [it_last, nq) of one head
+  int nq = uni((q_end - j0 + kQT - 1) / kQT);
+  if constexpr (WINDOW) {
+    const QueryTiles qt = query_tiles<128, kQT>(win, a.N, jt, segment);
+    it_last = uni(qt.lo);
+    nq = uni(qt.hi);
+    if (nq <= it_last) return;                        // no such segment
+  }
+  const int n_iter = nheads * (nq - it_last);
   const float c2 = a.scale_log2;
 
   // loop-invariant B operand of this wave's 32 keys: K^T (role A) or V^T (role B)
@@ -243,7 +256,8 @@ __device__ __forceinline__ void dkdv_workgroup(const KArgs& a, int T, const Deal
         char* Px = smem + kOffP + o_st * kPBufBytes + kb * 2 * kPBlockBytes + lane * 16;
         const int q0 = j0 + it * kQT;
         // tiles 0 and 1 touch the diagonal of the 128 keys, a partial last tile holds padding rows
-        const bool masked = it < 2 || (RAGGED && q0 + kQT > run.len);
+        const bool masked = it < 2 || (RAGGED && q0 + kQT > run.len) ||
+                            (WINDOW && q0 + kQT - 1 - j0 >= win.window && j0 + 127 >= win.sinks);
         // lse rows of both blocks (queries are register-indexed: 16 values per block and lane
         // half), fetched ahead of the scores so that the vector work below never waits on LDS
         float4 lr[2][4];
@@ -269,6 +283,7 @@ __device__ __forceinline__ void dkdv_workgroup(const KArgs& a, int T, const Deal
               if constexpr (MASKED) {
                 const int row = q0 + 32 * mb + 8 * vv + 4 * g32 + e;
                 if (key > row || (RAGGED && row >= run.len)) p = 0.f;
+                if (WINDOW && row - key >= win.window && key >= win.sinks) p = 0.f;
               }
               sx[4 * vv + e] = p;
             }
@@ -376,12 +391,15 @@ __device__ __forceinline__ void dkdv_workgroup(const KArgs& a, int T, const Deal
       q_st = q_st == 2 ? 0 : q_st + 1;
     } while (++n <= n_iter);
   }
-  if (a.dkv_partial) {   // contiguous fp32 partial of this part, summed by the combine pass
+  const bool cut = WINDOW && jt < win.sink_tiles;
+  if (a.dkv_partial || cut) {   // contiguous fp32 partial of this part (and segment), summed by the combine pass
     const size_t elems = (size_t)a.B * a.N * a.Hkv * 128;
     if (RAGGED && key >= run.len) return;   // padding key of a partial tile
     const int tok = token_of(run.p0 + key, s, a.N);
     float* dst = a.dkv_partial + (size_t)((role_b ? 0 : a.parts) + at.part) * elems +
                  ((size_t)((size_t)b * a.N + tok) * a.Hkv + c) * 128 + 4 * g32;
+    if constexpr (WINDOW)
+      if (cut) dst = far_row(win, a, role_b ? 0 : 1, at.part, segment, b, c, key, 128) + 4 * g32;
     const float mul = role_b ? a.scale : 1.f;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
@@ -412,6 +430,12 @@ __global__ void __launch_bounds__(512, 1)
 bwd_dkdv_split_kernel(KArgs a, int T, Deal deal, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[kSmemBytes];
   dkdv_workgroup<SPILL, RAGGED>(a, T, deal, first_block + block_id(), thread_id(), smem);
+}
+
+__global__ void __launch_bounds__(512, 1)
+window_dkdv_bf16_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[kSmemBytes];
+  dkdv_workgroup<false, true, true>(a, T, deal, first_block + block_id(), thread_id(), smem, win);
 }
 
 // Both in one launch (kv_first: dK/dV first): neither needs the other, and where one of them does not
@@ -446,6 +470,15 @@ int launch_bwd_dkdv_bf16(const KArgs& a, hipStream_t st) {
   if (a.ds_spill) return launch_blocks(bwd_dkdv_split_kernel<true, false>, g.blocks, 512, st, a, T, g.deal);
   if (a.ragged) return launch_blocks(bwd_dkdv_split_kernel<false, true>, g.blocks, 512, st, a, T, g.deal);
   return launch_blocks(bwd_dkdv_split_kernel<false, false>, g.blocks, 512, st, a, T, g.deal);
+}
+
+int launch_window_bwd_bf16(const KArgs& a, Win win, hipStream_t st) {
+  if (a.D == 64) return launch_window_bwd_d64(a, win, st);
+  const int T = ragged_tiles(a, 128), n_seq = a.B * a.Hkv * a.parts;
+  const Grid kv = grid_of(T, n_seq, 1, 32), q = grid_of(T, a.B * a.H, a.r, 64);
+  win.n_main = kv.blocks;
+  const int rc = launch_blocks(window_dkdv_bf16_kernel, kv.blocks + n_seq * win.sink_tiles * win.n_seg, 512, st, a, T, kv.deal, win);
+  return rc != 0 ? rc : launch_blocks(window_dq_bf16_kernel, q.blocks, 256, st, a, T, q.deal, win);
 }
 
 int launch_bwd_dq_bf16(const KArgs& a, hipStream_t st) {

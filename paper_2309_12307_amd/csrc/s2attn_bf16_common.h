@@ -200,6 +200,12 @@ __device__ __forceinline__ float sum_of_4(float x) {
   return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// Where a running maximum of raw scores starts: below any score, but finite also when scaled by c2: a masked score (-inf) is
+// then a zero in the first tile, any other a number that raises the maximum (or is as low as this).
+__device__ __forceinline__ float first_max(float c2) {
+  return c2 > 1.f ? -3.3e38f * __builtin_amdgcn_rcpf(c2) : -3.402823466e38f;
+}
+
 __device__ __forceinline__ bf16x8 pack8(float a0, float a1, float a2, float a3,
                                         float a4, float a5, float a6, float a7) {
   bf16x8 r;

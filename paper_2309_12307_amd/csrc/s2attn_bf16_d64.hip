@@ -13,6 +13,7 @@
 // out: forward 1516 -> 1236 us (matrix unit busy 54 % of the time at a clock of 1.6 GHz), dK/dV 3082 ->
 // 2198 us (51 % at 1.9 GHz), dQ 1866 -> 1542 us (64 % at 1.6 GHz, the power limit).
 #include "s2attn_bf16_common.h"
+#include "s2attn_bf16_tile64.h"
 #include "s2attn_device.h"
 #include "s2attn_launch.h"
 
@@ -20,47 +21,10 @@ namespace s2 {
 namespace {
 
 constexpr int DH = 64;
-constexpr int kRow = DH * 2;            // bytes of a tile row
+constexpr int kRow = kRow64;
 constexpr int kTR = 64;                 // rows per staged tile
 constexpr int kTile = kTR * kRow;       // 8 KB
 constexpr int kOwn = 128;               // rows a workgroup owns, 32 per wave
-
-// Tile rows 2R and 2R + 1 share the 256-byte LDS row R; its eight chunk columns are XOR-permuted
-// by a function of R mod 8 that takes every value (16 rows of one chunk column hit all banks) and
-// differs in bit 2 between neighbouring R (4 rows x 64 bytes of a transposing read do too).
-__device__ __forceinline__ int swz64(int R) { return ((R & 1) << 2) | ((R >> 1) & 3); }
-__device__ __forceinline__ int tile_off64(int row, int chunk) {
-  return (row >> 1) * 256 + ((row & 1) << 7) + ((chunk ^ swz64(row >> 1)) << 4);
-}
-
-struct Offsets64 {
-  int rm[4];      // row-major fragment k: elements [16k + 8g, +8) of row l % 32
-  int tr[2][2];   // transposed fragment, column block cb: rows 4g + L/4 and that + 8
-};
-__device__ __forceinline__ Offsets64 lane_offsets64(int lane) {
-  Offsets64 o;
-  const int l32 = lane & 31, g32 = lane >> 5, L = lane & 15;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) o.rm[k] = tile_off64(l32, 2 * k + g32);
-  const int row = 4 * g32 + (L >> 2);
-#pragma unroll
-  for (int cb = 0; cb < 2; ++cb) {
-    const int col = 32 * cb + (lane & 16) + 4 * (L & 3);
-    o.tr[cb][0] = tile_off64(row, col >> 3) + (col & 7) * 2;
-    o.tr[cb][1] = tile_off64(row + 8, col >> 3) + (col & 7) * 2;
-  }
-  return o;
-}
-template <int ROW0>   // a multiple of 16
-__device__ __forceinline__ bf16x8 rm64(const char* tile, const Offsets64& o, int k) {
-  return *reinterpret_cast<const bf16x8*>(tile + o.rm[k] + ROW0 * kRow);
-}
-template <int ROW0>
-__device__ __forceinline__ bf16x8 tr64(const char* tile, const Offsets64& o, int cb) {
-  const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(S2_LDS(bf16x4, tile + o.tr[cb][0] + ROW0 * kRow));
-  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(S2_LDS(bf16x4, tile + o.tr[cb][1] + ROW0 * kRow));
-  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
 
 // Staging of 64-row tiles of two tensors by four waves: wave w, pass p fills the 8 tile rows from
 // 8w + 32p (1 KB of LDS per tensor); a lane fetches the chunk that the layout places at its slot.
@@ -134,15 +98,14 @@ __device__ __forceinline__ void store_rows(const KArgs& a, void* out, const TStr
 // (120 registers).  Bound by the vector unit (153 instructions and 16 MFMAs per 64 x 32 tile) and
 // the clock it leaves.
 // ===========================================================================
-__global__ void __launch_bounds__(256, 4)
-fwd_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
-  __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];   // [stage][K,V]
-  fetch_args(a, deal);
+// WINDOW: one run of all tokens, key tiles of the sinks and of the window.  smem: [stage][K,V]
+template <bool WINDOW>
+__device__ __forceinline__ void fwd64_workgroup(const KArgs& a, int T, const Deal& deal, int block, const Win& win, char* smem) {
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
 
   int seq, rank;
-  if (!decode_block(first_block + block_id(), T, deal, seq, rank)) return;
+  if (!decode_block(block, T, deal, seq, rank)) return;
   const HeadPos at = head_of_seq(a, seq);
   const int c = at.c, b = at.b, h = at.h;
   int qt = T - 1 - rank;
@@ -152,7 +115,9 @@ fwd_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = uni(qt * kOwn);
   const int qw0 = i0 + 32 * w, qrow = qw0 + l32;
-  const int n_tiles = uni((min(run.len, i0 + kOwn) + kTR - 1) / kTR);
+  KeyTiles kt{};
+  if constexpr (WINDOW) kt = key_tiles<kTR>(win.window, win.sinks, i0, i0 + kOwn - 1, a.N);
+  const int n_tiles = WINDOW ? kt.total : uni((min(run.len, i0 + kOwn) + kTR - 1) / kTR);
   const float c2 = a.scale_log2;
 
   bf16x8 qf[4];
@@ -168,35 +133,36 @@ fwd_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
   const uint32_t base = lds_addr(smem);
   const Stager sg = stager(w, lane, k_rb, v_rb);
   auto issue = [&](int n, int stage) __attribute__((always_inline)) {
-    stage_pair(a, run, s, n * kTR, sg, w, k_head, k_rb, v_head, v_rb, base + stage * 2 * kTile,
+    stage_pair(a, run, s, (WINDOW ? kt.tile(n) : n) * kTR, sg, w, k_head, k_rb, v_head, v_rb, base + stage * 2 * kTile,
                base + stage * 2 * kTile + kTile);
   };
 
   const Offsets64 lo = lane_offsets64(lane);
   f32x16 o[2] = {zero16(), zero16()};
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = WINDOW ? first_max(c2) : -INFINITY, l_run = 0.f;
   issue(0, 0);
   for (int n = 0; n < n_tiles; ++n) {
     const int stage = n & 1;
     wait_vmcnt0();                        // this wave's part of tile n has landed
     __syncthreads();                      // everyone's part has landed; everyone left tile n - 1
     if (n + 1 < n_tiles) issue(n + 1, stage ^ 1);
-    const int j0 = n * kTR;
+    const int j0 = (WINDOW ? kt.tile(n) : n) * kTR;
     const char* Ks = smem + stage * 2 * kTile;
     const char* Vs = Ks + kTile;
     if (j0 > qw0 + 31) continue;          // beyond the diagonal of this wave's rows
+    if (WINDOW && (qw0 >= a.N || (j0 + kTR <= qw0 - win.window + 1 && j0 >= win.sinks))) continue;
     f32x16 s0 = zero16(), s1 = zero16();
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       s0 = mfma32(rm64<0>(Ks, lo, k), qf[k], s0);
       s1 = mfma32(rm64<32>(Ks, lo, k), qf[k], s1);
     }
-    if (j0 + kTR - 1 > qw0) {
+    if (j0 + kTR - 1 > qw0 || (WINDOW && j0 < qw0 + 31 - win.window + 1)) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int key = j0 + 8 * (v >> 2) + 4 * g32 + (v & 3);
-        if (key > qrow) s0[v] = -INFINITY;
-        if (key + 32 > qrow) s1[v] = -INFINITY;
+        if (key > qrow || (WINDOW && qrow - key >= win.window && key >= win.sinks)) s0[v] = -INFINITY;
+        if (key + 32 > qrow || (WINDOW && qrow - key - 32 >= win.window && key + 32 >= win.sinks)) s1[v] = -INFINITY;
       }
     }
     // online softmax: the maximum is raised (and O rescaled) only when it grows by more than 2^8
@@ -247,6 +213,19 @@ fwd_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
   if (g32 == 0 && qrow < run.len)
     a.lse[((size_t)b * a.H + h) * a.N + token_of(run.p0 + qrow, s, a.N)] =
         (m_run * c2 + __builtin_amdgcn_logf(l_tot)) * kLn2;
+}
+
+__global__ void __launch_bounds__(256, 4)
+fwd_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];
+  fetch_args(a, deal);
+  fwd64_workgroup<false>(a, T, deal, first_block + block_id(), Win{}, smem);
+}
+
+__global__ void __launch_bounds__(256, 4)
+window_fwd_d64_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];
+  fwd64_workgroup<true>(a, T, deal, first_block + block_id(), win, smem);
 }
 
 // ===========================================================================
@@ -308,9 +287,9 @@ __device__ __forceinline__ void ac_mma64(const bf16x8 (&buf)[8], const bf16x8 (&
 }
 // P and dS of a block as B operands.  MASK: keys after the query, and query rows at or past q_lim
 // (padding of a partial tile), give zero.
-template <int MB, bool MASK>
+template <int MB, bool MASK, bool WINDOW = false>
 __device__ __forceinline__ void softmax64(Block64& x, const RowTerms& rows, bf16x8 (&pf)[2], bf16x8 (&df)[2], float c2,
-                                          int g32, int q_first = 0, int key = 0, int q_lim = 0) {
+                                          int g32, int q_first = 0, int key = 0, int q_lim = 0, const Win& win = Win{}) {
 #pragma unroll
   for (int vv = 0; vv < 4; ++vv) {
     const float4 l4 = *reinterpret_cast<const float4*>(&rows.lse2[32 * MB + 8 * vv + 4 * g32]);
@@ -322,6 +301,7 @@ __device__ __forceinline__ void softmax64(Block64& x, const RowTerms& rows, bf16
       if (MASK) {
         const int q = q_first + 32 * MB + 8 * vv + 4 * g32 + e;
         if (key > q || q >= q_lim) p = 0.f;
+        if (WINDOW && q - key >= win.window && key >= win.sinks) p = 0.f;
       }
       x.s[v] = p;
       x.dp[v] *= p;
@@ -365,28 +345,33 @@ __device__ __forceinline__ void dkdv64_tile(const char* Qs, const char* dOs, con
   __builtin_amdgcn_sched_barrier(0);
 }
 // One 32-query block by itself (tiles on the diagonal, the partial last tile).
-template <int MB>
+template <int MB, bool WINDOW>
 __device__ __forceinline__ void dkdv64_masked(const char* Qs, const char* dOs, const RowTerms& rows, const Offsets64& lo,
                                               const bf16x8 (&kf)[4], const bf16x8 (&vf)[4], f32x16 (&dk)[2],
-                                              f32x16 (&dv)[2], float c2, int g32, int q_first, int key, int q_lim) {
+                                              f32x16 (&dv)[2], float c2, int g32, int q_first, int key, int q_lim, const Win& win) {
   bf16x8 f[8], pf[2], df[2];
   Block64 x;
   sc_load64<MB>(f, Qs, dOs, lo);
   dp_init64<MB>(x, rows, g32);
   sc_mma64(f, x, kf, vf);
   ac_load64<MB>(f, Qs, dOs, lo);
-  softmax64<MB, true>(x, rows, pf, df, c2, g32, q_first, key, q_lim);
+  softmax64<MB, true, WINDOW>(x, rows, pf, df, c2, g32, q_first, key, q_lim, win);
   ac_mma64(f, pf, df, dk, dv);
 }
 
-// smem: [stage][Q,dO]
+// smem: [stage][Q,dO].  WINDOW: one run of all tokens, the query tiles that meet the keys' windows (query_tiles).
+template <bool WINDOW>
 __device__ __forceinline__ void dkdv64_workgroup(const KArgs& a, int T, const Deal& deal, int block, int tid, char* smem,
-                                                 RowTerms (&rows_s)[2]) {
+                                                 RowTerms (&rows_s)[2], const Win& win = Win{}) {
   const int lane = tid & 63, w = uni(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
 
-  int seq, jt;
-  if (!decode_block(block, T, deal, seq, jt)) return;
+  int seq, jt, segment = 0;
+  if constexpr (WINDOW) {
+    if (!decode_window(win, block, T, deal, seq, jt, segment)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, jt)) return;
+  }
   const KvPos at = kv_of_seq(a, seq);
   const int c = at.c, b = at.b;
   int h_lo, nheads, s;
@@ -397,8 +382,15 @@ __device__ __forceinline__ void dkdv64_workgroup(const KArgs& a, int T, const De
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int j0 = uni(jt * kOwn);
   const int kw0 = j0 + 32 * w, key = kw0 + l32;
-  const int nq = uni((run.len - j0 + kTR - 1) / kTR);   // query tiles of one head
-  const int n_iter = nheads * nq;
+  int it_last = 0;                                      // query tiles [it_last, nq) of one head
+  int nq = uni((run.len - j0 + kTR - 1) / kTR);
+  if constexpr (WINDOW) {
+    const QueryTiles qt = query_tiles<kOwn, kTR>(win, a.N, jt, segment);
+    it_last = uni(qt.lo);
+    nq = uni(qt.hi);
+    if (nq <= it_last) return;                          // no such segment
+  }
+  const int n_iter = nheads * (nq - it_last);
   const float c2 = a.scale_log2;
 
   bf16x8 kf[4], vf[4];   // K^T and V^T of this wave's keys
@@ -448,28 +440,40 @@ __device__ __forceinline__ void dkdv64_workgroup(const KArgs& a, int T, const De
       const char* Qs = smem + (n & 1) * 2 * kTile;
       // blocks before this wave's keys see none of them; rows >= run.len are padding
       if (q0 + 31 >= kw0)
-        dkdv64_masked<0>(Qs, Qs + kTile, rows_s[n & 1], lo, kf, vf, dk, dv, c2, g32, q0, key, run.len);
+        dkdv64_masked<0, WINDOW>(Qs, Qs + kTile, rows_s[n & 1], lo, kf, vf, dk, dv, c2, g32, q0, key, run.len, win);
       if (q0 + 63 >= kw0)
-        dkdv64_masked<1>(Qs, Qs + kTile, rows_s[n & 1], lo, kf, vf, dk, dv, c2, g32, q0, key, run.len);
+        dkdv64_masked<1, WINDOW>(Qs, Qs + kTile, rows_s[n & 1], lo, kf, vf, dk, dv, c2, g32, q0, key, run.len, win);
     }
   };
   int it = nq - 1;
-  if (run.len % kTR != 0 && it >= 2) masked_tiles(it--);
-  for (; it >= 2; --it)
+  if constexpr (WINDOW) {
+    // the run's last tile, and those in which a query's window ends after a key (beyond the sinks)
+    while (it >= max(2, it_last) && (j0 + (it + 1) * kTR > run.len || ((it + 1) * kTR - 1 >= win.window && j0 + kOwn - 1 >= win.sinks)))
+      masked_tiles(it--);
+  } else {
+    if (run.len % kTR != 0 && it >= 2) masked_tiles(it--);
+  }
+  for (; it >= max(2, it_last); --it)
     for (int hh = 0; hh < nheads; ++hh, ++n) {
       begin_tile(n, hh, it);
       const char* Qs = smem + (n & 1) * 2 * kTile;
       dkdv64_tile(Qs, Qs + kTile, rows_s[n & 1], lo, kf, vf, dk, dv, c2, g32);
     }
-  for (; it >= 0; --it) masked_tiles(it);
+  for (; it >= it_last; --it) masked_tiles(it);
   __syncthreads();
 
-  if (a.dkv_partial) {   // query heads cut into parts: fp32 partial of this one, summed by the combine pass
+  const bool cut = WINDOW && jt < win.sink_tiles;
+  if (a.dkv_partial || cut) {   // query heads cut into parts: fp32 partial of this one, summed by the combine pass
     if (key >= run.len) return;
     const size_t elems = (size_t)a.B * a.N * a.Hkv * DH;
     const int tok = token_of(run.p0 + key, s, a.N);
     float* dk_out = a.dkv_partial + (size_t)at.part * elems + ((size_t)((size_t)b * a.N + tok) * a.Hkv + c) * DH + 4 * g32;
     float* dv_out = dk_out + (size_t)a.parts * elems;
+    if constexpr (WINDOW)
+      if (cut) {
+        dk_out = far_row(win, a, 0, at.part, segment, b, c, key, kOwn) + 4 * g32;
+        dv_out = far_row(win, a, 1, at.part, segment, b, c, key, kOwn) + 4 * g32;
+      }
 #pragma unroll
     for (int db = 0; db < 2; ++db)
 #pragma unroll
@@ -494,10 +498,10 @@ __device__ __forceinline__ void dkdv64_workgroup(const KArgs& a, int T, const De
 // dQ: 128 query rows a workgroup (32 per wave), 64-key tiles up to the diagonal, S and dP
 // recomputed.  Three workgroups per CU (156 registers).
 // ===========================================================================
-template <int ROW0>
+template <int ROW0, bool WINDOW>
 __device__ __forceinline__ void dq64_block(const char* Ks, const char* Vs, const Offsets64& lo, const bf16x8 (&qf)[4],
                                            const bf16x8 (&dof)[4], const f32x16& neg_delta, f32x16 (&dq)[2], float c2,
-                                           float lse2, int j0, int qrow, int g32, bool masked) {
+                                           float lse2, int j0, int qrow, int g32, bool masked, const Win& win) {
   f32x16 sx = zero16(), dp = neg_delta;   // dP - delta
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -506,8 +510,10 @@ __device__ __forceinline__ void dq64_block(const char* Ks, const char* Vs, const
   }
   if (masked) {
 #pragma unroll
-    for (int v = 0; v < 16; ++v)
-      if (j0 + ROW0 + 8 * (v >> 2) + 4 * g32 + (v & 3) > qrow) sx[v] = -INFINITY;
+    for (int v = 0; v < 16; ++v) {
+      const int key = j0 + ROW0 + 8 * (v >> 2) + 4 * g32 + (v & 3);
+      if (key > qrow || (WINDOW && qrow - key >= win.window && key >= win.sinks)) sx[v] = -INFINITY;
+    }
   }
 #pragma unroll
   for (int v = 0; v < 16; ++v) dp[v] *= __builtin_amdgcn_exp2f(fmaf(sx[v], c2, -lse2));
@@ -521,7 +527,9 @@ __device__ __forceinline__ void dq64_block(const char* Ks, const char* Vs, const
 }
 
 // smem: [stage][K,V]
-__device__ __forceinline__ void dq64_workgroup(const KArgs& a, int T, const Deal& deal, int block, int tid, char* smem) {
+template <bool WINDOW>
+__device__ __forceinline__ void dq64_workgroup(const KArgs& a, int T, const Deal& deal, int block, int tid, char* smem,
+                                               const Win& win = Win{}) {
   const int lane = tid & 63, w = uni(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
 
@@ -536,7 +544,9 @@ __device__ __forceinline__ void dq64_workgroup(const KArgs& a, int T, const Deal
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = uni(qt * kOwn);
   const int qw0 = i0 + 32 * w, qrow = qw0 + l32;
-  const int n_tiles = uni((min(run.len, i0 + kOwn) + kTR - 1) / kTR);
+  KeyTiles kt{};
+  if constexpr (WINDOW) kt = key_tiles<kTR>(win.window, win.sinks, i0, i0 + kOwn - 1, a.N);
+  const int n_tiles = WINDOW ? kt.total : uni((min(run.len, i0 + kOwn) + kTR - 1) / kTR);
   const float c2 = a.scale_log2;
 
   bf16x8 qf[4], dof[4];
@@ -560,7 +570,7 @@ __device__ __forceinline__ void dq64_workgroup(const KArgs& a, int T, const Deal
   const uint32_t base = lds_addr(smem);
   const Stager sg = stager(w, lane, k_rb, v_rb);
   auto issue = [&](int n, int stage) __attribute__((always_inline)) {
-    stage_pair(a, run, s, n * kTR, sg, w, k_head, k_rb, v_head, v_rb, base + stage * 2 * kTile,
+    stage_pair(a, run, s, (WINDOW ? kt.tile(n) : n) * kTR, sg, w, k_head, k_rb, v_head, v_rb, base + stage * 2 * kTile,
                base + stage * 2 * kTile + kTile);
   };
 
@@ -572,13 +582,14 @@ __device__ __forceinline__ void dq64_workgroup(const KArgs& a, int T, const Deal
     wait_vmcnt0();
     __syncthreads();
     if (n + 1 < n_tiles) issue(n + 1, stage ^ 1);
-    const int j0 = n * kTR;
+    const int j0 = (WINDOW ? kt.tile(n) : n) * kTR;
     const char* Ks = smem + stage * 2 * kTile;
     const char* Vs = Ks + kTile;
     if (j0 > qw0 + 31) continue;
-    const bool masked = j0 + kTR - 1 > qw0;
-    dq64_block<0>(Ks, Vs, lo, qf, dof, neg_delta, dq, c2, lse2, j0, qrow, g32, masked);
-    dq64_block<32>(Ks, Vs, lo, qf, dof, neg_delta, dq, c2, lse2, j0, qrow, g32, masked);
+    if (WINDOW && (qw0 >= a.N || (j0 + kTR <= qw0 - win.window + 1 && j0 >= win.sinks))) continue;
+    const bool masked = j0 + kTR - 1 > qw0 || (WINDOW && j0 < qw0 + 31 - win.window + 1);
+    dq64_block<0, WINDOW>(Ks, Vs, lo, qf, dof, neg_delta, dq, c2, lse2, j0, qrow, g32, masked, win);
+    dq64_block<32, WINDOW>(Ks, Vs, lo, qf, dof, neg_delta, dq, c2, lse2, j0, qrow, g32, masked, win);
   }
   __syncthreads();
   char* region = smem + w * 32 * kRow;
@@ -591,13 +602,25 @@ __global__ void __launch_bounds__(256, 2)
 bwd_dkdv_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];
   __shared__ __attribute__((aligned(1024))) RowTerms rows_s[2];
-  dkdv64_workgroup(a, T, deal, first_block + block_id(), thread_id(), smem, rows_s);
+  dkdv64_workgroup<false>(a, T, deal, first_block + block_id(), thread_id(), smem, rows_s);
 }
 
 __global__ void __launch_bounds__(256, 3)
 bwd_dq_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];
-  dq64_workgroup(a, T, deal, first_block + block_id(), thread_id(), smem);
+  dq64_workgroup<false>(a, T, deal, first_block + block_id(), thread_id(), smem);
+}
+
+// The same under a window, always in one launch.
+__global__ void __launch_bounds__(256, 2)
+window_bwd_d64_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];
+  __shared__ __attribute__((aligned(1024))) RowTerms rows_s[2];
+  const int block = first_block + block_id();
+  if (block < n_kv)
+    dkdv64_workgroup<true>(a, T, deal_kv, block, thread_id(), smem, rows_s, win);
+  else
+    dq64_workgroup<true>(a, T, deal_q, block - n_kv, thread_id(), smem, win);
 }
 
 // Both in one launch, dK/dV first: neither needs the other, and where they do not fill the chip their
@@ -607,9 +630,9 @@ bwd_both_d64_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q) {
   __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];
   __shared__ __attribute__((aligned(1024))) RowTerms rows_s[2];
   if (block_id() < n_kv)
-    dkdv64_workgroup(a, T, deal_kv, block_id(), thread_id(), smem, rows_s);
+    dkdv64_workgroup<false>(a, T, deal_kv, block_id(), thread_id(), smem, rows_s);
   else
-    dq64_workgroup(a, T, deal_q, block_id() - n_kv, thread_id(), smem);
+    dq64_workgroup<false>(a, T, deal_q, block_id() - n_kv, thread_id(), smem);
 }
 
 }  // namespace
@@ -618,6 +641,20 @@ int launch_fwd_d64(const KArgs& a, hipStream_t st) {
   const int T = ragged_tiles(a, kOwn);
   const Grid g = grid_of(T, a.B * a.H * a.NG, a.r, 128);   // 32 CUs per XCD, four workgroups each
   return launch_blocks(fwd_d64_kernel, g.blocks, 256, st, a, T, g.deal);
+}
+
+int launch_window_fwd_d64(const KArgs& a, const Win& win, hipStream_t st) {
+  const int T = ragged_tiles(a, kOwn);
+  const Grid g = grid_of(T, a.B * a.H, a.r, 128);
+  return launch_blocks(window_fwd_d64_kernel, g.blocks, 256, st, a, T, g.deal, win);
+}
+
+int launch_window_bwd_d64(const KArgs& a, Win win, hipStream_t st) {
+  const int T = ragged_tiles(a, kOwn), n_seq = a.B * a.Hkv * a.parts;
+  const Grid kv = grid_of(T, n_seq, 1, 64), q = grid_of(T, a.B * a.H, a.r, 64);
+  win.n_main = kv.blocks;
+  const int n_kv = pad_to(kv.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
+  return launch_blocks(window_bwd_d64_kernel, n_kv + q.blocks, 256, st, a, n_kv, T, kv.deal, q.deal, win);
 }
 
 int launch_bwd_dkdv_d64(const KArgs& a, hipStream_t st) {

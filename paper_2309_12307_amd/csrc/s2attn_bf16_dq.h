@@ -64,14 +64,14 @@ __device__ __forceinline__ void dq_mma(const bf16x8 (&buf)[4], const bf16x8 (&qf
 }
 
 // dS^T = P^T * (dP^T - delta) of one 32-key block, packed as two B operands.
-template <int ROW0>
+template <int ROW0, bool WINDOW>
 __device__ __forceinline__ void dq_ds(f32x16& sa, const f32x16& pa, bf16x8& ds_lo, bf16x8& ds_hi, int j0, int qrow,
-                                      float c2, float lse2, float delta, int g32, bool masked) {
-  if (masked) {   // wave-uniform: exp2(-inf) = 0 removes keys after the query
+                                      float c2, float lse2, float delta, int g32, bool masked, const Win& win) {
+  if (masked) {   // wave-uniform: exp2(-inf) = 0 removes keys after the query, or before its window
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int key = j0 + ROW0 + 8 * (v >> 2) + 4 * g32 + (v & 3);
-      if (key > qrow) sa[v] = -INFINITY;
+      if (key > qrow || (WINDOW && qrow - key >= win.window && key >= win.sinks)) sa[v] = -INFINITY;
     }
   }
 #pragma unroll
@@ -80,10 +80,10 @@ __device__ __forceinline__ void dq_ds(f32x16& sa, const f32x16& pa, bf16x8& ds_l
   ds_hi = pack8(sa[8], sa[9], sa[10], sa[11], sa[12], sa[13], sa[14], sa[15]);
 }
 
-template <bool XTR>
+template <bool XTR, bool WINDOW>
 __device__ __forceinline__ void dq_tile(f32x16 (&dq_acc)[4], const bf16x8 (&qf)[8], const bf16x8 (&dof)[8],
                                         const char* Ks, const char* Vs, const LaneOffsets& lo, int j0,
-                                        int qrow, float c2, float lse2, float delta, int g32, bool masked) {
+                                        int qrow, float c2, float lse2, float delta, int g32, bool masked, const Win& win) {
 #define S2_DQ_STEP(N, CUR, NXT)                                   \
   dq_load<N + 1, XTR>(NXT, Ks, Vs, lo, tr0);                      \
   dq_mma<N>(CUR, qf, dof, sa, pa, dsf, dq_acc);                   \
@@ -101,7 +101,7 @@ __device__ __forceinline__ void dq_tile(f32x16 (&dq_acc)[4], const bf16x8 (&qf)[
   S2_DQ_STEP(1, fb, fa);
   S2_DQ_STEP(2, fa, fb);
   S2_DQ_STEP(3, fb, fa);            // loads step 4 (block 1) before the vector section
-  dq_ds<0>(sa, pa, dsf[0], dsf[1], j0, qrow, c2, lse2, delta, g32, masked);
+  dq_ds<0, WINDOW>(sa, pa, dsf[0], dsf[1], j0, qrow, c2, lse2, delta, g32, masked, win);
   sa = zero16();
   pa = zero16();
   __builtin_amdgcn_sched_barrier(0);
@@ -109,7 +109,7 @@ __device__ __forceinline__ void dq_tile(f32x16 (&dq_acc)[4], const bf16x8 (&qf)[
   S2_DQ_STEP(5, fb, fa);
   S2_DQ_STEP(6, fa, fb);
   S2_DQ_STEP(7, fb, fa);            // loads step 8 (first K^T fragments)
-  dq_ds<32>(sa, pa, dsf[2], dsf[3], j0, qrow, c2, lse2, delta, g32, masked);
+  dq_ds<32, WINDOW>(sa, pa, dsf[2], dsf[3], j0, qrow, c2, lse2, delta, g32, masked, win);
   __builtin_amdgcn_sched_barrier(0);
   S2_DQ_STEP(8, fa, fb);
   S2_DQ_STEP(9, fb, fa);
@@ -119,9 +119,11 @@ __device__ __forceinline__ void dq_tile(f32x16 (&dq_acc)[4], const bf16x8 (&qf)[
 }
 
 // smem: [2 stages][K,V] tiles, afterwards one 8 KB block per wave.  RAGGED: as in the forward
-// kernels, and any tile that runs past the end of a group.
-template <bool RAGGED, int WAVES>
-__device__ __forceinline__ void dq_workgroup(const KArgs& a, int T, const Deal& deal, int block, int tid, char* smem) {
+// kernels, and any tile that runs past the end of a group.  WINDOW (with RAGGED): one run of all tokens, key tiles of the
+// sinks and of the window.
+template <bool RAGGED, int WAVES, bool WINDOW = false>
+__device__ __forceinline__ void dq_workgroup(const KArgs& a, int T, const Deal& deal, int block, int tid, char* smem,
+                                             const Win& win = Win{}) {
   constexpr int BM = 32 * WAVES;
   constexpr int kPassRows = 4 * WAVES;   // tile rows that the workgroup stages with one load per wave
 
@@ -202,22 +204,30 @@ __device__ __forceinline__ void dq_workgroup(const KArgs& a, int T, const Deal& 
 #pragma unroll
   for (int db = 0; db < 4; ++db) dq_acc[db] = zero16();
 
-  issue_tile(jt_first, 0);
-  const int n_tiles = (RAGGED ? uni((min(i0 + BM, run.len) + BN - 1) / BN) : (i0 + BM) / BN) - jt_first;
+  KeyTiles kt{};
+  if constexpr (WINDOW) kt = key_tiles<BN>(win.window, win.sinks, i0, i0 + BM - 1, a.N);
+  issue_tile(WINDOW ? kt.tile(0) : jt_first, 0);
+  const int n_tiles = WINDOW ? kt.total : (RAGGED ? uni((min(i0 + BM, run.len) + BN - 1) / BN) : (i0 + BM) / BN) - jt_first;
   // With four waves the stage is a compile-time constant of the body (the loop is unrolled by the
   // number of stages), so every LDS read is lane offset + immediate; in the kernel that shares its
   // registers with dK/dV that spills.
   auto body = [&](auto stage_c, int n) __attribute__((always_inline)) {
     const int STAGE = stage_c;
-    const int jt = jt_first + n;
+    const int jt = WINDOW ? kt.tile(n) : jt_first + n;
     wait_vmcnt0();
     __syncthreads();
-    if (n + 1 < n_tiles) issue_tile(jt + 1, STAGE ^ 1);
+    if (n + 1 < n_tiles) issue_tile(WINDOW ? kt.tile(n + 1) : jt + 1, STAGE ^ 1);
     const int j0 = jt * BN;
     const char* Ks = smem + STAGE * 2 * kTileBytes;
     const char* Vs = Ks + kTileBytes;
+    if constexpr (WINDOW) {
+      if (j0 > qw0 + 31 || qw0 >= a.N || (j0 + BN <= qw0 - win.window + 1 && j0 >= win.sinks)) return;
+      dq_tile<false, true>(dq_acc, qf, dof, Ks, Vs, lo, j0, qrow, c2, lse2, delta, g32,
+                           j0 + BN - 1 > qw0 || j0 < qw0 + 31 - win.window + 1, win);
+      return;
+    }
     if (j0 > qw0 + 31 || j0 + BN - 1 < lo_w) return;   // wholly outside this wave's visible keys
-    dq_tile<RAGGED && WAVES == 8>(dq_acc, qf, dof, Ks, Vs, lo, j0, qrow, c2, lse2, delta, g32, j0 + BN - 1 > qw0);
+    dq_tile<RAGGED && WAVES == 8, false>(dq_acc, qf, dof, Ks, Vs, lo, j0, qrow, c2, lse2, delta, g32, j0 + BN - 1 > qw0, win);
   };
   if constexpr (WAVES == 4) {
     for (int n = 0; n < n_tiles; n += 2) {
@@ -241,6 +251,12 @@ __global__ void __launch_bounds__(256, 2)
 bwd_dq_bf16_kernel(KArgs a, int T, Deal deal, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[4 * kTileBytes];
   dq_workgroup<RAGGED, 4>(a, T, deal, first_block + block_id(), thread_id(), smem);
+}
+
+__global__ void __launch_bounds__(256, 2)
+window_dq_bf16_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * kTileBytes];
+  dq_workgroup<true, 4, true>(a, T, deal, first_block + block_id(), thread_id(), smem, win);
 }
 
 }  // namespace

@@ -138,6 +138,17 @@ __device__ __forceinline__ void fwd_tile(FwdState& st, const bf16x8 (&qf)[8], co
   fwd_pv(st, Vs, lo, pf);
 }
 
+// Removes what query row `qrow` does not see under a window.
+__device__ __forceinline__ void mask_window(f32x16& s0, f32x16& s1, int j0, int qrow, const Win& win, int g32) {
+  const int first = qrow - win.window + 1;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    const int key = j0 + 8 * (v >> 2) + 4 * g32 + (v & 3);
+    if (key > qrow || (key < first && key >= win.sinks)) s0[v] = -INFINITY;
+    if (key + 32 > qrow || (key + 32 < first && key + 32 >= win.sinks)) s1[v] = -INFINITY;
+  }
+}
+
 // Normalises a wave's 32 x 128 output block, transposes it through the wave's private
 // 8 KB LDS region and stores it (and lse) at the un-rolled token rows.
 template <bool RAGGED>
@@ -165,13 +176,10 @@ __device__ __forceinline__ void fwd_epilogue(const KArgs& a, FwdState& st, char*
 // tiles may be partial and the wrap point may fall inside one; the rows of such a tile find
 // their tokens one by one, all other tiles are 64 consecutive tokens.  The two halves of a
 // split wrap-around group run as causal runs of their own (run_of_tile).
-template <bool RAGGED>
-__global__ void __launch_bounds__(256, 2)
-fwd_bf16_kernel(KArgs a, int T, Deal deal, int first_block) {
+// WINDOW (with RAGGED): one run of all tokens, key tiles of the sinks and of the window.
+template <bool RAGGED, bool WINDOW>
+__device__ __forceinline__ void fwd_workgroup(const KArgs& a, int T, const Deal& deal, int block, const Win& win, char* smem) {
   constexpr int BM = 128;
-  __shared__ __attribute__((aligned(1024))) char smem[4 * kTileBytes];   // [stage][K,V]
-  fetch_args(a, deal);
-
   const int tid = thread_id(), lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
 
@@ -182,7 +190,7 @@ fwd_bf16_kernel(KArgs a, int T, Deal deal, int first_block) {
   // four of the eight XCDs only (N = 8192, H = 32, G = 2048: forward 278 us,
   // 149 dealt out per query head; dQ 383 and 198).
   int seq, rank;
-  if (!decode_block(first_block + block_id(), T, deal, seq, rank)) return;
+  if (!decode_block(block, T, deal, seq, rank)) return;
   const HeadPos at = head_of_seq(a, seq);
   const int gidx = at.g, c = at.c, b = at.b, h = at.h;
   int qt = T - 1 - rank;
@@ -261,6 +269,30 @@ fwd_bf16_kernel(KArgs a, int T, Deal deal, int first_block) {
 #pragma unroll
   for (int db = 0; db < 4; ++db) st.o_acc[db] = zero16();
 
+  if constexpr (WINDOW) {
+    st.m_run = first_max(c2);   // a row may see nothing of the first tiles
+    const KeyTiles kt = key_tiles<BN>(win.window, win.sinks, i0, i0 + BM - 1, a.N);
+    issue_tile(kt.tile(0), 0);
+    for (int n = 0; n < kt.total; ++n) {
+      const int stage = n & 1, j0 = kt.tile(n) * BN;
+      wait_vmcnt0();
+      __syncthreads();
+      if (n + 1 < kt.total) issue_tile(kt.tile(n + 1), stage ^ 1);
+      const char* Ks = smem + stage * 2 * kTileBytes;
+      // after the wave's rows, or between the sinks and their windows
+      if (j0 > qw0 + 31 || qw0 >= a.N || (j0 + BN <= qw0 - win.window + 1 && j0 >= win.sinks)) continue;
+      f32x16 s0, s1;
+      bf16x8 pf[4];
+      fwd_scores(s0, s1, qf, Ks, lo, j0, qrow, g32, false);
+      if (j0 + BN - 1 > qw0 || j0 < qw0 + 31 - win.window + 1) mask_window(s0, s1, j0, qrow, win, g32);
+      fwd_softmax(st, s0, s1, c2, pf);
+      fwd_pv(st, Ks + kTileBytes, lo, pf);
+    }
+    __syncthreads();
+    fwd_epilogue<RAGGED>(a, st, smem + w * (32 * kRowBytes), b, h, run, s, qw0, c2, lane, l32, g32);
+    return;
+  }
+
   issue_tile(jt_first, 0);
   const int n_tiles = jt_diag + 2 - jt_first;
   for (int n = 0; n < n_tiles; ++n) {
@@ -281,6 +313,20 @@ fwd_bf16_kernel(KArgs a, int T, Deal deal, int first_block) {
 
   // ---- epilogue: normalise, transpose through LDS, store at un-rolled token rows
   fwd_epilogue<RAGGED>(a, st, smem + w * (32 * kRowBytes), b, h, run, s, qw0, c2, lane, l32, g32);
+}
+
+template <bool RAGGED>
+__global__ void __launch_bounds__(256, 2)
+fwd_bf16_kernel(KArgs a, int T, Deal deal, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * kTileBytes];   // [stage][K,V]
+  fetch_args(a, deal);
+  fwd_workgroup<RAGGED, false>(a, T, deal, first_block + block_id(), Win{}, smem);
+}
+
+__global__ void __launch_bounds__(256, 2)
+window_fwd_bf16_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * kTileBytes];
+  fwd_workgroup<true, true>(a, T, deal, first_block + block_id(), win, smem);
 }
 
 // ---- the matrix block of the eight-wave kernel as 8 steps of 4 MFMAs, each fed by 4
@@ -418,9 +464,7 @@ fwd_bf16_pp_kernel(KArgs a, int T, Deal deal) {
   LaneOffsets lo;
   init_lane_offsets(lo, lane);
   FwdState st;
-  // below any score, but finite also when scaled: a masked score (-inf) is then a zero in the first tile, any other
-  // a number that raises the maximum (or is as low as this)
-  st.m_run = c2 > 1.f ? -3.3e38f * __builtin_amdgcn_rcpf(c2) : -3.402823466e38f;
+  st.m_run = first_max(c2);
   st.l_run = 0.f;
 #pragma unroll
   for (int db = 0; db < 4; ++db) st.o_acc[db] = zero16();
@@ -505,6 +549,13 @@ fwd_bf16_pp_kernel(KArgs a, int T, Deal deal) {
 }
 
 }  // namespace
+
+int launch_window_fwd_bf16(const KArgs& a, const Win& win, hipStream_t st) {
+  if (a.D == 64) return launch_window_fwd_d64(a, win, st);
+  const int T = ragged_tiles(a, 128);
+  const Grid g = grid_of(T, a.B * a.H, a.r, 64);
+  return launch_blocks(window_fwd_bf16_kernel, g.blocks, 256, st, a, T, g.deal, win);
+}
 
 int launch_fwd_bf16(const KArgs& a, hipStream_t st) {
   if (a.D == 64) return launch_fwd_d64(a, st);

@@ -186,6 +186,67 @@ __device__ __forceinline__ void part_heads(const KArgs& a, int c, int part, int&
   shift = lo >= a.shifted_from ? a.shift : 0;
 }
 
+// ---- visible keys under a window: position p sees key j iff j <= p and (p - j < window or j < sinks).
+
+// Tiles of TK keys that rows at positions p_lo .. p_hi see: n_sink tiles from key 0 on, then those from `first` on.
+struct KeyTiles {
+  int n_sink, first, total, end;   // end: no key at or after it is visible
+  __device__ __forceinline__ int tile(int n) const { return n < n_sink ? n : first + n - n_sink; }
+};
+template <int TK>
+__device__ __forceinline__ KeyTiles key_tiles(int window, int sinks, int p_lo, int p_hi, int keys) {
+  KeyTiles t;
+  t.end = max(min(p_hi, keys - 1) + 1, 0);
+  const int lo = window > 0 ? max(p_lo - window + 1, 0) : 0;
+  t.first = lo / TK;
+  t.n_sink = min((min(sinks, t.end) + TK - 1) / TK, t.first);
+  t.total = t.n_sink + max((t.end + TK - 1) / TK - t.first, 0);
+  return t;
+}
+
+// Attention with a window and sinks on contiguous tensors: one causal run [0, N) a head, no shift.  dK/dV of the first keys, which
+// all later queries see, is cut into segments of query tiles: segment 0 holds those that meet the key tile's windows,
+// the others seg_tiles tiles each.  What the segments add up goes to `partial`, fp32
+// [dk, dv][part][segment][B][Hkv][sink_tiles * keys of a tile][D], and is summed by a pass of its own.
+struct Win {
+  int window, sinks;
+  int sink_tiles, n_seg, seg_tiles;   // key tiles that are cut (0: none, their workgroups take all queries), segments but 0
+  int n_main;                         // blocks of segment 0; those of the others follow
+  Div by_far, by_seg;                 // sink_tiles * n_seg, n_seg
+  float* partial;
+};
+
+// Query tiles [lo, hi) of QT rows, counted from key j0 on, of key tile jt = j0 / KT.
+struct QueryTiles {
+  int lo, hi;
+};
+template <int KT, int QT>
+__device__ __forceinline__ QueryTiles query_tiles(const Win& win, int N, int jt, int segment) {
+  const int all = (N - jt * KT + QT - 1) / QT, main = min(all, (KT - 1 + win.window + QT - 1) / QT);
+  if (jt >= win.sink_tiles) return QueryTiles{0, jt * KT < win.sinks ? all : main};
+  if (segment == 0) return QueryTiles{0, main};
+  const int lo = main + (segment - 1) * win.seg_tiles;
+  return QueryTiles{lo, min(all, lo + win.seg_tiles)};
+}
+
+// Block -> (sequence, key tile, segment) of dK/dV.
+__device__ __forceinline__ bool decode_window(const Win& win, int block, int T, const Deal& deal, int& seq, int& jt, int& segment) {
+  segment = 0;
+  if (block < win.n_main) return decode_block(block, T, deal, seq, jt);
+  const int far = block - win.n_main;
+  seq = quot(far, win.by_far);
+  const int x = far - seq * win.sink_tiles * win.n_seg;
+  jt = quot(x, win.by_seg);
+  segment = 1 + x - jt * win.n_seg;
+  return seq < deal.n_seq;
+}
+
+// Row of the partial dk (which = 0) or dv (1) of a segment.
+__device__ __forceinline__ float* far_row(const Win& win, const KArgs& a, int which, int part, int segment, int b, int c, int key, int KT) {
+  const size_t slots = (size_t)a.parts * (1 + win.n_seg), slot = (size_t)part * (1 + win.n_seg) + segment;
+  return win.partial + ((((which * slots + slot) * a.B + b) * a.Hkv + c) * ((size_t)win.sink_tiles * KT) + key) * a.D;
+}
+
 // ---- dS hand-over between the two backward kernels (tile-aligned shapes only).
 // The dK/dV kernel stores dS = P * (dP - delta) of every (64 queries x 128 keys) tile it
 // visits as one 16 KB blob, exactly as its waves hold it: [key block kb 0..3][operand f 0..3]

@@ -31,89 +31,11 @@
 #include "s2attn_bf16_common.h"
 #include "s2attn_device.h"
 #include "s2attn_f32_common.h"
+#include "s2attn_f32_tile.h"
 #include "s2attn_launch.h"
 
 namespace s2 {
 namespace {
-
-constexpr int kTile = 32;     // rows of a staged tile
-constexpr int kWgRows = 64;   // rows a workgroup owns: 16 per wave
-
-template <int D>
-struct Lanes {
-  static constexpr int kRow = D * 4;             // bytes of a tile row
-  static constexpr int kTileBytes = kTile * kRow;
-  int rm[2];   // row-major operand: byte offset for even / odd i, + 128 (i / 2)
-  int tr[4];   // transposed operand of register v, + 256 j
-  int st_row;  // staging: tile row of this lane's first 16 bytes, and its chunk
-  int st_chunk;
-
-  __device__ __forceinline__ void init(int lane, int w) {
-    const int c16 = lane & 15, q4 = lane >> 4;
-    rm[0] = c16 * kRow + ((q4 ^ (c16 & 7)) << 4);
-    rm[1] = c16 * kRow + (((4 + q4) ^ (c16 & 7)) << 4);
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int row = 4 * q4 + v;
-      tr[v] = row * kRow + ((c16 ^ (row & 7)) << 4);
-    }
-    constexpr int kChunks = D / 4;               // 16-byte chunks of a row: 16 or 32
-    constexpr int kRowsPer = 64 / kChunks;       // rows one wave instruction fills: 4 or 2
-    st_row = w * kRowsPer + lane / kChunks;
-    st_chunk = (lane % kChunks) ^ (st_row & 7);
-  }
-
-  // X[16 RB + c16][16 i + 4 q4 ..]
-  template <int RB>
-  __device__ __forceinline__ f32x4 row(const char* tile, int i) const {
-    return *reinterpret_cast<const f32x4*>(tile + rm[i & 1] + 16 * RB * kRow + 128 * (i >> 1));
-  }
-  // X[16 RB + 4 q4 + v][64 j + 4 c16 ..]
-  template <int RB>
-  __device__ __forceinline__ f32x4 col(const char* tile, int v, int j) const {
-    return *reinterpret_cast<const f32x4*>(tile + tr[v] + 16 * RB * kRow + 256 * j);
-  }
-
-  // Stages rows i0 .. i0 + 31 of a run (clamped to its last row) of one head.
-  __device__ __forceinline__ void stage(const KArgs& a, const Run& run, int s, const void* src, const TStride& st,
-                                        int b, int head, int i0, uint32_t lds, int w) const {
-    constexpr int kStep = 4 * (64 / (D / 4));    // rows the four waves fill together: 16 or 8
-#pragma unroll
-    for (int p = 0; p < kTile / kStep; ++p) {
-      const int tok = run_token(a, run, i0 + p * kStep + st_row, s);
-      dma16(static_cast<const char*>(src) + row_off(st, b, tok, head) * 4 + (st_chunk << 4), lds + (p * 4 + w) * 1024);
-    }
-  }
-};
-
-// acc[RB] += rows of the tile (16 RB + c16) against the wave's own 16 rows held in `own`.
-template <int D>
-__device__ __forceinline__ void scores(f32x4 (&acc)[2], const char* tile, const Lanes<D>& ln, const f32x4 (&own)[D / 16]) {
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    const f32x4 x0 = ln.template row<0>(tile, i), x1 = ln.template row<1>(tile, i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[0] = mfma4(x0[e], own[i][e], acc[0]);
-      acc[1] = mfma4(x1[e], own[i][e], acc[1]);
-    }
-  }
-}
-
-// acc[j][e] += X^T W for the 32 rows of a tile: W = P or dS as it stands in the accumulators.
-template <int D>
-__device__ __forceinline__ void accumulate(f32x4 (&acc)[D / 64][4], const char* tile, const Lanes<D>& ln, const f32x4 (&wt)[2]) {
-#pragma unroll
-  for (int v = 0; v < 4; ++v)
-#pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-      const f32x4 x0 = ln.template col<0>(tile, v, j), x1 = ln.template col<1>(tile, v, j);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[j][e] = mfma4(x0[e], wt[0][v], acc[j][e]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[j][e] = mfma4(x1[e], wt[1][v], acc[j][e]);
-    }
-}
 
 // ---------------------------------------------------------------------------
 // Forward.  A workgroup (4 waves) owns 64 query rows of one causal run, a wave 16 of them
@@ -121,16 +43,14 @@ __device__ __forceinline__ void accumulate(f32x4 (&acc)[D / 64][4], const char* 
 // 64 rows and not 128: at D = 128 two such workgroups share a CU's LDS (64 KB each), and a
 // layer of a few hundred tokens still spreads over the chip.
 // ---------------------------------------------------------------------------
-template <int D>
-__global__ void __launch_bounds__(256, 2) fwd_f32_kernel(KArgs a, int T, Deal deal, int first_block) {
+// WINDOW: one run of all tokens, key tiles of the sinks and of the window.  smem: [stage][K, V]
+template <int D, bool WINDOW>
+__device__ __forceinline__ void fwd_f32_workgroup(const KArgs& a, int T, const Deal& deal, int block, const Win& win, char* smem) {
   using L = Lanes<D>;
-  __shared__ __attribute__((aligned(1024))) char smem[4 * L::kTileBytes];   // [stage][K, V]
-  fetch_args(a, deal);
-
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
   int seq, rank;
-  if (!decode_block(first_block + block_id(), T, deal, seq, rank)) return;
+  if (!decode_block(block, T, deal, seq, rank)) return;
   const HeadPos at = head_of_seq(a, seq);
   const int s = uni(shift_of_head(a, at.h));
   Run run;
@@ -145,10 +65,13 @@ __global__ void __launch_bounds__(256, 2) fwd_f32_kernel(KArgs a, int T, Deal de
   L ln;
   ln.init(lane, w);
   const uint32_t base = lds_addr(smem);
+  KeyTiles kt{};
+  if constexpr (WINDOW) kt = key_tiles<kTile>(win.window, win.sinks, i0, i0 + kWgRows - 1, a.N);
   auto issue_tile = [&](int n) __attribute__((always_inline)) {
     const uint32_t dst = base + (n & 1) * 2 * L::kTileBytes;
-    ln.stage(a, run, s, a.k, a.sk, at.b, at.c, n * kTile, dst, w);
-    ln.stage(a, run, s, a.v, a.sv, at.b, at.c, n * kTile, dst + L::kTileBytes, w);
+    const int first = (WINDOW ? kt.tile(n) : n) * kTile;
+    ln.stage(a, run, s, a.k, a.sk, at.b, at.c, first, dst, w);
+    ln.stage(a, run, s, a.v, a.sv, at.b, at.c, first, dst + L::kTileBytes, w);
   };
   issue_tile(0);
   f32x4 qf[D / 16];
@@ -164,25 +87,27 @@ __global__ void __launch_bounds__(256, 2) fwd_f32_kernel(KArgs a, int T, Deal de
   // exp2(-inf) = 0 and goes on with its later keys (from -inf they would be exp2(-inf + inf) = NaN)
   float m_run = -FLT_MAX, l_run = 0.f;
 
-  const int n_tiles = uni((min(i0 + kWgRows, run.len) - 1) / kTile + 1);
+  const int n_tiles = WINDOW ? kt.total : uni((min(i0 + kWgRows, run.len) - 1) / kTile + 1);
   for (int n = 0; n < n_tiles; ++n) {
     wait_vmcnt0();
     __syncthreads();
     if (n + 1 < n_tiles) issue_tile(n + 1);
-    const int j0 = n * kTile;
+    const int j0 = (WINDOW ? kt.tile(n) : n) * kTile;
+    if (WINDOW && j0 + kTile <= qw0 - win.window + 1 && j0 >= win.sinks) continue;
     if (j0 > qw0 + 15 || qw0 >= run.len) continue;   // wholly after this wave's queries, or no query at all
     const char* Ks = smem + (n & 1) * 2 * L::kTileBytes;
     const char* Vs = Ks + L::kTileBytes;
     f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
     scores<D>(sc, Ks, ln, qf);
-    const bool masked = j0 + kTile - 1 > qw0;
+    const bool masked = j0 + kTile - 1 > qw0 || (WINDOW && j0 < qw0 + 15 - win.window + 1);
     float mx = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         float x = sc[kb][v] * c2;
-        if (masked && j0 + 16 * kb + 4 * q4 + v > qrow) x = -INFINITY;
+        const int key = j0 + 16 * kb + 4 * q4 + v;
+        if (masked && (key > qrow || (WINDOW && qrow - key >= win.window && key >= win.sinks))) x = -INFINITY;
         sc[kb][v] = x;
         mx = fmaxf(mx, x);
       }
@@ -213,6 +138,19 @@ __global__ void __launch_bounds__(256, 2) fwd_f32_kernel(KArgs a, int T, Deal de
   if (q4 == 0) a.lse[((size_t)at.b * a.H + at.h) * a.N + tok] = (m_run + log2f(l_tot)) * kLn2;
 }
 
+template <int D>
+__global__ void __launch_bounds__(256, 2) fwd_f32_kernel(KArgs a, int T, Deal deal, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * Lanes<D>::kTileBytes];
+  fetch_args(a, deal);
+  fwd_f32_workgroup<D, false>(a, T, deal, first_block + block_id(), Win{}, smem);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) window_fwd_f32_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * Lanes<D>::kTileBytes];
+  fwd_f32_workgroup<D, true>(a, T, deal, first_block + block_id(), win, smem);
+}
+
 // ---------------------------------------------------------------------------
 // Backward, one launch: the first n_kv blocks are dK/dV workgroups, the others dQ workgroups
 // (independent of each other, and a small layer fills the chip with neither alone).
@@ -226,13 +164,20 @@ __global__ void __launch_bounds__(256, 2) fwd_f32_kernel(KArgs a, int T, Deal de
 // while the matrix unit works on the present one, which costs an O tile from L2 per query tile
 // of 16 k MFMA cycles.  A launch saved is what counts at the small sizes.
 // ---------------------------------------------------------------------------
-template <int D>
-__device__ __forceinline__ void bwd_dkdv_block(const KArgs& a, char* smem, float* rows_s, int block, int T, const Deal& deal) {
+// WINDOW: one run of all tokens; dK/dV takes the query tiles that meet the keys' windows (query_tiles), dQ the key tiles of
+// the sinks and of the window.
+template <int D, bool WINDOW>
+__device__ __forceinline__ void bwd_dkdv_block(const KArgs& a, char* smem, float* rows_s, int block, int T, const Deal& deal,
+                                               const Win& win) {
   using L = Lanes<D>;
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, kt;
-  if (!decode_block(block, T, deal, seq, kt)) return;   // key tile 0 is the heaviest
+  int seq, kt, segment = 0;
+  if constexpr (WINDOW) {
+    if (!decode_window(win, block, T, deal, seq, kt, segment)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, kt)) return;   // key tile 0 is the heaviest
+  }
   const KvPos at = kv_of_seq(a, seq);
   int h_lo, nheads, s;
   part_heads(a, at.c, at.part, h_lo, nheads, s);
@@ -242,7 +187,13 @@ __device__ __forceinline__ void bwd_dkdv_block(const KArgs& a, char* smem, float
   const int j0 = uni(kt * kWgRows);
   const int kw0 = j0 + 16 * w, key = kw0 + c16;
   const int tok = run_token(a, run, key, s);
-  const int it_first = j0 / kTile, it_last = uni((run.len - 1) / kTile);
+  int it_first = j0 / kTile, it_last = uni((run.len - 1) / kTile);
+  if constexpr (WINDOW) {
+    const QueryTiles qt = query_tiles<kWgRows, kTile>(win, a.N, kt, segment);
+    it_last = uni(it_first + qt.hi - 1);
+    it_first = uni(it_first + qt.lo);
+    if (it_last < it_first) return;                       // no such segment
+  }
   const int n_iter = nheads * (it_last - it_first + 1);
   const float c2 = a.scale_log2;
 
@@ -318,7 +269,8 @@ __device__ __forceinline__ void bwd_dkdv_block(const KArgs& a, char* smem, float
       }
       scores<D>(sc, Qs, ln, kf);
       scores<D>(dp, dOs, ln, vf);
-      const bool masked = kw0 + 15 > q0 || q0 + kTile > run.len;
+      const bool masked = kw0 + 15 > q0 || q0 + kTile > run.len ||
+                          (WINDOW && q0 + kTile - 1 - kw0 >= win.window && kw0 + 15 >= win.sinks);
 #pragma unroll
       for (int qb = 0; qb < 2; ++qb) {
         const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + 16 * qb);
@@ -326,7 +278,7 @@ __device__ __forceinline__ void bwd_dkdv_block(const KArgs& a, char* smem, float
         for (int v = 0; v < 4; ++v) {
           const int i = q0 + 16 * qb + 4 * q4 + v;
           float p = exp2f(fmaf(sc[qb][v], c2, -l4[v]));
-          if (masked && (key > i || i >= run.len)) p = 0.f;
+          if (masked && (key > i || i >= run.len || (WINDOW && i - key >= win.window && key >= win.sinks))) p = 0.f;
           sc[qb][v] = p;
           dp[qb][v] *= p;
         }
@@ -338,6 +290,13 @@ __device__ __forceinline__ void bwd_dkdv_block(const KArgs& a, char* smem, float
   }
 
   if (key >= run.len) return;
+  if constexpr (WINDOW) {
+    if (kt < win.sink_tiles) {
+      store_row<D>(far_row(win, a, 0, at.part, segment, at.b, at.c, key, kWgRows), dk, a.scale, q4);
+      store_row<D>(far_row(win, a, 1, at.part, segment, at.b, at.c, key, kWgRows), dv, 1.f, q4);
+      return;
+    }
+  }
   if (a.dkv_partial) {   // contiguous fp32 partial of this part, summed by the combine pass
     const size_t elems = (size_t)a.B * a.N * a.Hkv * D;
     float* dst = a.dkv_partial + at.part * elems + ((size_t)((size_t)at.b * a.N + tok) * a.Hkv + at.c) * D;
@@ -349,8 +308,8 @@ __device__ __forceinline__ void bwd_dkdv_block(const KArgs& a, char* smem, float
   }
 }
 
-template <int D>
-__device__ __forceinline__ void bwd_dq_block(const KArgs& a, char* smem, int block, int T, const Deal& deal) {
+template <int D, bool WINDOW>
+__device__ __forceinline__ void bwd_dq_block(const KArgs& a, char* smem, int block, int T, const Deal& deal, const Win& win) {
   using L = Lanes<D>;
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
@@ -370,10 +329,13 @@ __device__ __forceinline__ void bwd_dq_block(const KArgs& a, char* smem, int blo
   L ln;
   ln.init(lane, w);
   const uint32_t base = lds_addr(smem);
+  KeyTiles kt{};
+  if constexpr (WINDOW) kt = key_tiles<kTile>(win.window, win.sinks, i0, i0 + kWgRows - 1, a.N);
   auto issue_tile = [&](int n) __attribute__((always_inline)) {
     const uint32_t dst = base + (n & 1) * 2 * L::kTileBytes;
-    ln.stage(a, run, s, a.k, a.sk, at.b, at.c, n * kTile, dst, w);
-    ln.stage(a, run, s, a.v, a.sv, at.b, at.c, n * kTile, dst + L::kTileBytes, w);
+    const int first = (WINDOW ? kt.tile(n) : n) * kTile;
+    ln.stage(a, run, s, a.k, a.sk, at.b, at.c, first, dst, w);
+    ln.stage(a, run, s, a.v, a.sv, at.b, at.c, first, dst + L::kTileBytes, w);
   };
   issue_tile(0);
   f32x4 qf[D / 16], gf[D / 16], dq[D / 64][4];
@@ -395,12 +357,13 @@ __device__ __forceinline__ void bwd_dq_block(const KArgs& a, char* smem, int blo
 #pragma unroll
     for (int e = 0; e < 4; ++e) dq[j][e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int n_tiles = uni((min(i0 + kWgRows, run.len) - 1) / kTile + 1);
+  const int n_tiles = WINDOW ? kt.total : uni((min(i0 + kWgRows, run.len) - 1) / kTile + 1);
   for (int n = 0; n < n_tiles; ++n) {
     wait_vmcnt0();
     __syncthreads();
     if (n + 1 < n_tiles) issue_tile(n + 1);
-    const int j0 = n * kTile;
+    const int j0 = (WINDOW ? kt.tile(n) : n) * kTile;
+    if (WINDOW && j0 + kTile <= qw0 - win.window + 1 && j0 >= win.sinks) continue;
     if (j0 > qw0 + 15 || qw0 >= run.len) continue;
     const char* Ks = smem + (n & 1) * 2 * L::kTileBytes;
     const char* Vs = Ks + L::kTileBytes;
@@ -412,13 +375,14 @@ __device__ __forceinline__ void bwd_dq_block(const KArgs& a, char* smem, int blo
     }
     scores<D>(sc, Ks, ln, qf);
     scores<D>(dp, Vs, ln, gf);
-    const bool masked = j0 + kTile - 1 > qw0;
+    const bool masked = j0 + kTile - 1 > qw0 || (WINDOW && j0 < qw0 + 15 - win.window + 1);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         float p = exp2f(fmaf(sc[kb][v], c2, -lse2));
-        if (masked && j0 + 16 * kb + 4 * q4 + v > qrow) p = 0.f;
+        const int key = j0 + 16 * kb + 4 * q4 + v;
+        if (masked && (key > qrow || (WINDOW && qrow - key >= win.window && key >= win.sinks))) p = 0.f;
         dp[kb][v] *= p;
       }
     accumulate<D>(dq, Ks, ln, dp);
@@ -434,9 +398,21 @@ bwd_f32_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, int first_bl
   __shared__ __attribute__((aligned(16))) float rows_s[2 * 2 * kTile];             // [stage][lse * log2(e), delta]
   const int block = first_block + block_id();
   if (block < n_kv)
-    bwd_dkdv_block<D>(a, smem, rows_s, block, T, deal_kv);
+    bwd_dkdv_block<D, false>(a, smem, rows_s, block, T, deal_kv, Win{});
   else
-    bwd_dq_block<D>(a, smem, block - n_kv, T, deal_q);
+    bwd_dq_block<D, false>(a, smem, block - n_kv, T, deal_q, Win{});
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2)
+window_bwd_f32_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * Lanes<D>::kTileBytes];
+  __shared__ __attribute__((aligned(16))) float rows_s[2 * 2 * kTile];
+  const int block = first_block + block_id();
+  if (block < n_kv)
+    bwd_dkdv_block<D, true>(a, smem, rows_s, block, T, deal_kv, win);
+  else
+    bwd_dq_block<D, true>(a, smem, block - n_kv, T, deal_q, win);
 }
 
 template <int D>
@@ -444,6 +420,22 @@ int launch_fwd_t(const KArgs& a, hipStream_t st) {
   const int T = ragged_tiles(a, kWgRows);
   const Grid g = grid_of(T, a.B * a.H * a.NG, a.r, 64);
   return launch_blocks(fwd_f32_kernel<D>, g.blocks, 256, st, a, T, g.deal);
+}
+
+template <int D>
+int launch_window_fwd_t(const KArgs& a, const Win& win, hipStream_t st) {
+  const int T = ragged_tiles(a, kWgRows);
+  const Grid g = grid_of(T, a.B * a.H, a.r, 64);
+  return launch_blocks(window_fwd_f32_kernel<D>, g.blocks, 256, st, a, T, g.deal, win);
+}
+
+template <int D>
+int launch_window_bwd_t(const KArgs& a, Win win, hipStream_t st) {
+  const int T = ragged_tiles(a, kWgRows), n_seq = a.B * a.Hkv * a.parts;
+  const Grid kv = grid_of(T, n_seq, 1, 64), q = grid_of(T, a.B * a.H, a.r, 64);
+  win.n_main = kv.blocks;
+  const int n_kv = pad_to(kv.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
+  return launch_blocks(window_bwd_f32_kernel<D>, n_kv + q.blocks, 256, st, a, n_kv, T, kv.deal, q.deal, win);
 }
 
 template <int D>
@@ -488,6 +480,14 @@ bool small_bwd(const KArgs& a) {
 }
 
 }  // namespace
+
+int launch_window_fwd_f32(const KArgs& a, const Win& win, hipStream_t st) {
+  return a.D == 64 ? launch_window_fwd_t<64>(a, win, st) : launch_window_fwd_t<128>(a, win, st);
+}
+
+int launch_window_bwd_f32(const KArgs& a, const Win& win, hipStream_t st) {
+  return a.D == 64 ? launch_window_bwd_t<64>(a, win, st) : launch_window_bwd_t<128>(a, win, st);
+}
 
 int launch_fwd_f32(const KArgs& a, hipStream_t st) {
   if (small_fwd(a)) return launch_fwd_f32_small(a, st);

@@ -37,6 +37,26 @@ int launch_delta_bf16(const KArgs& a, hipStream_t st);
 // dk = sum of the partials of all parts (same for dv), cast to the output type
 int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st);
 
+// Window attention: forward; dK/dV and dQ (bf16: delta must be ready), dk, dv of cut key tiles left as partials; their sum
+int launch_window_fwd_f32(const KArgs& a, const Win& win, hipStream_t st);
+int launch_window_bwd_f32(const KArgs& a, const Win& win, hipStream_t st);
+int launch_window_fwd_bf16(const KArgs& a, const Win& win, hipStream_t st);
+int launch_window_bwd_bf16(const KArgs& a, Win win, hipStream_t st);
+int launch_window_fwd_d64(const KArgs& a, const Win& win, hipStream_t st);
+int launch_window_bwd_d64(const KArgs& a, Win win, hipStream_t st);
+int launch_sink_combine(const KArgs& a, const Win& win, int dtype, hipStream_t st);
+
+// current device is gfx950: an S2ATTN_* code
+int check_device();
+
+// Paged cache (s2attn_paged.h).  `cache` is the cache's S2ATTN_* type
+struct PArgs;
+int launch_cache_write(const PArgs& a, int D, int dtype, int cache, hipStream_t st);
+int launch_cache_read(const PArgs& a, int D, int dtype, int cache, hipStream_t st);
+int launch_paged_bf16(const PArgs& a, int D, int cache, int blocks, hipStream_t st);
+int launch_paged_f32(const PArgs& a, int D, int cache, int blocks, hipStream_t st);
+int launch_paged_join(const PArgs& a, int D, bool bf16, hipStream_t st);   // splits > 1: after one of the two
+
 // Number of tile sequences walked together (see decode_block) for a kernel whose XCD holds
 // `slots` workgroups at a time, and the sequence count padded to a multiple of it.
 inline int interleave_for(int T, int slots) { return T >= slots ? 1 : (slots + T - 1) / T; }

@@ -1,0 +1,110 @@
+// What the kernels of the paged cache share: the argument block, how a block finds its sequence and how a key
+// position finds its row in the cache.
+//
+// Nothing that these kernels read from the device is trusted with an address: row_start is clamped to [0, T], key positions
+// stay below table_cols * page_size, and a page number outside [0, pages) stands for no page (its keys are invisible).
+#pragma once
+#include "s2attn_device.h"
+
+namespace s2 {
+
+struct PArgs {
+  const void* q; void* o; float* lse;          // (T,H,D), (T,H,D), (H,T) or null
+  void* k; void* v;                            // rows of the call, (T,Hkv,D): written to the cache or read from it
+  char* kc; char* vc;                          // cache, (pages, page_size, Hkv, D)
+  uint8_t* ke; uint8_t* ve;                    // e4m3: biased exponents, (pages, page_size, Hkv)
+  const int* table; const int* row_start; const int* kv_len;
+  float* part_o; float* part_lse;              // splits > 1: [split][T][H][D] and [split][T][H] (base 2)
+  long long q_t, q_h, k_t, k_h, v_t, v_h;      // strides in elements
+  long long kc_p, kc_t, kc_h, vc_p, vc_t, vc_h;
+  long long ke_p, ke_t, ke_h, ve_p, ve_t, ve_h;
+  long long table_b;
+  int T, B, H, Hkv, r, pages, page_size, max_keys;   // max_keys: table_cols * page_size
+  int window, sinks;                           // window 0: every earlier key is visible
+  int splits, min_tiles;                       // most pieces the keys of a row tile are cut into; fewest key tiles of one
+  int n_tiles;                                 // row tiles of the launch (tile_of_block)
+  Div by_r, by_page, by_tiles, by_groups;
+  float scale_log2;
+};
+
+__device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ __forceinline__ int start_of(const PArgs& a, int i) { return min(max(a.row_start[i], 0), a.T); }
+
+// Rows of sequence b: packed rows s0 .. s0 + n - 1, the positions kv - n .. kv - 1; keys: cached positions that exist.
+struct SeqRows {
+  int b, s0, n, kv, keys;
+};
+__device__ __forceinline__ SeqRows seq_rows(const PArgs& a, int b) {
+  SeqRows s;
+  s.b = b;
+  s.s0 = start_of(a, b);
+  s.n = max(start_of(a, b + 1) - s.s0, 0);
+  s.kv = max(a.kv_len[b], 0);
+  s.keys = min(s.kv, a.max_keys);
+  return s;
+}
+
+// The number of sequences whose first unit is at or before `id`, less one: units are packed rows (SHIFT < 0) or row
+// tiles of 2^SHIFT (token, query head of the kv head) pairs, of which sequence b owns those from
+// (row_start[b] * r >> SHIFT) + b on: at least as many as it needs, and no running sum is needed to place them.
+// The whole wave calls it: 64 sequences a step, one answer.
+template <int SHIFT>
+__device__ __forceinline__ int first_tile(const PArgs& a, int b) { return (int)((unsigned)(start_of(a, b) * a.r) >> SHIFT) + b; }
+template <int SHIFT>
+__device__ __forceinline__ int find_seq(const PArgs& a, int id, int lane) {
+  int n = 0;
+  for (int i0 = 0; i0 < a.B; i0 += 64) {
+    const int i = i0 + lane;
+    bool before = false;
+    if (i < a.B) {
+      if constexpr (SHIFT < 0) before = start_of(a, i) <= id;
+      else before = first_tile<SHIFT>(a, i) <= id;
+    }
+    n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+  }
+  return wave_uniform(n - 1);
+}
+
+// Block -> (row tile, kv head, split).  Blocks of one (kv head, split) read the same keys: whole such groups go to an XCD
+// where they divide among the eight, row tiles from the last (most keys) to the first.
+__device__ __forceinline__ bool tile_of_block(const PArgs& a, int block, int& tile, int& c, int& split) {
+  const int groups = a.Hkv * a.splits;
+  int g;
+  if ((groups & 7) == 0) {
+    const int slot = block >> 3, u = quot(slot, a.by_tiles);
+    g = u * 8 + (block & 7);
+    tile = slot - u * a.n_tiles;
+  } else {
+    tile = quot(block, a.by_groups);
+    g = block - tile * groups;
+  }
+  tile = a.n_tiles - 1 - tile;
+  split = g / a.Hkv;
+  c = g - split * a.Hkv;
+  return tile >= 0 && g < groups;
+}
+
+// Key tiles of a piece, and the pieces that `total` tiles make: at most `splits`, none of fewer than min_tiles tiles
+// (but the last).
+__device__ __forceinline__ int tiles_of_split(const PArgs& a, int total) { return max((total + a.splits - 1) / a.splits, a.min_tiles); }
+
+// The cache row of key position j: page number (-1: none) and place in the page.
+struct CacheRow {
+  int page, at;
+};
+__device__ __forceinline__ CacheRow cache_row(const PArgs& a, int b, int j, int end) {
+  CacheRow x{-1, 0};
+  if (j >= 0 && j < end) {
+    const int slot = quot(j, a.by_page);
+    x.at = j - slot * a.page_size;
+    const int page = a.table[b * a.table_b + slot];
+    x.page = (unsigned)page < (unsigned)a.pages ? page : -1;
+  }
+  return x;
+}
+
+// A wave's 16 bytes that stand for a row that is not there.
+static __device__ const uint4 zero_row[32] = {};
+
+}  // namespace s2

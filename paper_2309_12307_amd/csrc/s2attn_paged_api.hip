@@ -1,0 +1,220 @@
+// Host side of the paged cache's entry points (include/s2attn.h): argument checks, how finely the keys are dealt out,
+// and launches.  Nothing here allocates device memory.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstring>
+
+#include "s2attn.h"
+#include "s2attn_launch.h"
+#include "s2attn_paged.h"
+
+namespace {
+
+constexpr size_t kAlign = 256;
+constexpr long long kMost = 1LL << 30;   // key positions of a sequence, (row, head) pairs of a call
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+struct Axis {
+  long long stride, extent;
+};
+
+// Strides of a tensor whose axes have these extents, the contiguous ones where all are zero; `last` elements are
+// contiguous.
+template <int N>
+void resolve(const long long (&st)[N], const long long (&extent)[N], long long last, long long (&out)[N]) {
+  bool zero = true;
+  for (long long x : st) zero = zero && x == 0;
+  long long step = last;
+  for (int i = N - 1; i >= 0; --i) {
+    out[i] = zero ? step : st[i];
+    step *= extent[i];
+  }
+}
+
+// No stride negative, off `align` or too long for 64-bit offsets; distinct rows in distinct places where `disjoint`.
+template <int N>
+bool strides_ok(const long long (&st)[N], const long long (&extent)[N], long long last, int align, bool disjoint) {
+  long long s[N];
+  resolve(st, extent, last, s);
+  Axis ax[N];
+  for (int i = 0; i < N; ++i) {
+    if (s[i] < 0 || s[i] % align != 0 || s[i] >= (1LL << 40)) return false;
+    if (extent[i] > 1 && (double)s[i] * extent[i] > 4.0e18) return false;
+    ax[i] = Axis{s[i], extent[i]};
+  }
+  if (!disjoint) return true;
+  std::sort(ax, ax + N, [](const Axis& x, const Axis& y) { return x.stride < y.stride; });
+  long long span = last;
+  for (const Axis& x : ax) {
+    if (x.extent <= 1) continue;
+    if (x.stride < span) return false;
+    span = x.stride * (x.extent - 1) + span;
+  }
+  return true;
+}
+
+int bytes_of(int dtype) { return dtype == S2ATTN_F32 ? 4 : dtype == S2ATTN_BF16 ? 2 : 1; }
+
+bool shape_valid(const s2attn_paged_params* p) {
+  return p->T >= 0 && p->B > 0 && p->H > 0 && p->Hkv > 0 && p->D > 0 && p->pages > 0 && p->page_size > 0 && p->table_cols > 0;
+}
+
+// Rows of a row tile of the attention kernels, as a power of two, and keys of a key tile.
+int tile_log2(const s2attn_paged_params* p) { return p->dtype == S2ATTN_F32 ? 6 : 7; }
+int tile_keys(const s2attn_paged_params* p) { return p->dtype == S2ATTN_F32 ? 32 : 64; }
+
+long long row_tiles(const s2attn_paged_params* p) { return (((long long)p->T * (p->H / p->Hkv)) >> tile_log2(p)) + p->B; }
+
+// How the keys of a row tile are dealt out: at most `splits` pieces of min_tiles key tiles or more.
+struct Pieces {
+  int splits, min_tiles;
+};
+Pieces pieces_wanted(const s2attn_paged_params* p) {
+  const int TK = tile_keys(p);
+  const long long most = (long long)p->table_cols * p->page_size;
+  const long long rows = (long long)p->T * (p->H / p->Hkv), seqs = std::max(1, std::min(p->B, p->T));
+  const long long tile = 1LL << tile_log2(p), in_tile = std::min(tile, (rows + seqs - 1) / seqs);
+  const long long blocks = std::max<long long>(1, std::max((rows + tile - 1) / tile, seqs) * p->Hkv);
+  long long keys = p->max_kv > 0 ? std::min<long long>(p->max_kv, most) : most;
+  if (p->window > 0) keys = std::min<long long>(keys, (long long)p->window + p->sinks + (rows + seqs - 1) / seqs + 2 * TK);
+  const long long min_keys = std::max<long long>(256, 32 * in_tile);
+  const long long target = in_tile <= 16 ? 4096 : 512;
+  long long splits = std::min((keys + min_keys - 1) / min_keys, (target + blocks - 1) / blocks);
+  splits = std::max<long long>(1, std::min<long long>(splits, 256));
+  return Pieces{(int)splits, (int)(min_keys / TK)};
+}
+
+size_t piece_bytes(const s2attn_paged_params* p) { return (size_t)p->T * p->H * (p->D + 1) * sizeof(float); }
+
+int check(const s2attn_paged_params* p, int call) {
+  if (!p) return S2ATTN_ERR_NULL;
+  if (call < S2ATTN_PAGED_WRITE || call > S2ATTN_PAGED_FWD) return S2ATTN_ERR_DTYPE;
+  const bool fwd = call == S2ATTN_PAGED_FWD;
+  if (p->dtype != S2ATTN_BF16 && p->dtype != S2ATTN_F32) return S2ATTN_ERR_DTYPE;
+  if (p->cache_dtype != p->dtype && p->cache_dtype != S2ATTN_E4M3) return S2ATTN_ERR_DTYPE;
+  const int H = fwd ? p->H : p->Hkv;
+  if (p->T < 0 || p->B <= 0 || H <= 0 || p->Hkv <= 0 || p->D <= 0 || p->pages <= 0 || p->page_size <= 0 || p->table_cols <= 0)
+    return S2ATTN_ERR_DIM;
+  if (H % p->Hkv != 0) return S2ATTN_ERR_HEADS;
+  if (p->D != 64 && p->D != 128) return S2ATTN_ERR_HEADDIM;
+  if (fwd && (p->window < 0 || p->sinks < 0 || p->max_kv < 0)) return S2ATTN_ERR_WINDOW;
+  // positions, (row, head) pairs and block numbers are non-negative ints; a wave's pieces of a row are counted in them too
+  if ((long long)p->table_cols * p->page_size > kMost || (long long)p->T * H > kMost || p->Hkv > 65536) return S2ATTN_ERR_TOO_LARGE;
+  if ((long long)p->T * p->Hkv > kMost / 8 || p->B > (1 << 24)) return S2ATTN_ERR_TOO_LARGE;
+  if (fwd && row_tiles(p) * p->Hkv > kMost) return S2ATTN_ERR_TOO_LARGE;
+
+  const int row_align = 16 / bytes_of(p->dtype), cache_align = 16 / bytes_of(p->cache_dtype);
+  const long long cache_ext[3] = {p->pages, p->page_size, p->Hkv}, kv_ext[2] = {p->T, p->Hkv}, q_ext[2] = {p->T, H};
+  const bool write = call == S2ATTN_PAGED_WRITE, read = call == S2ATTN_PAGED_READ, e4m3 = p->cache_dtype == S2ATTN_E4M3;
+  if (!strides_ok(p->k_cache_strides, cache_ext, p->D, cache_align, write) || !strides_ok(p->v_cache_strides, cache_ext, p->D, cache_align, write))
+    return S2ATTN_ERR_STRIDE;
+  if (e4m3 && (!strides_ok(p->k_exp_strides, cache_ext, 1, 1, write) || !strides_ok(p->v_exp_strides, cache_ext, 1, 1, write)))
+    return S2ATTN_ERR_STRIDE;
+  if (p->table_stride != 0 && p->B > 1 && (p->table_stride < 0 || p->table_stride >= (1LL << 40))) return S2ATTN_ERR_STRIDE;
+  if (fwd ? !strides_ok(p->q_strides, q_ext, p->D, row_align, false)
+          : !strides_ok(p->k_strides, kv_ext, p->D, row_align, read) || !strides_ok(p->v_strides, kv_ext, p->D, row_align, read))
+    return S2ATTN_ERR_STRIDE;
+  for (const void* x : {(const void*)p->page_table, (const void*)p->row_start, (const void*)p->kv_len}) {
+    if (!x) return S2ATTN_ERR_NULL;
+    if (!aligned(x, 4)) return S2ATTN_ERR_ALIGN;
+  }
+  for (const void* x : {p->k_cache, p->v_cache}) {
+    if (!x) return S2ATTN_ERR_NULL;
+    if (!aligned(x, 16)) return S2ATTN_ERR_ALIGN;
+  }
+  if (e4m3 && (!p->k_exp || !p->v_exp)) return S2ATTN_ERR_NULL;
+  if (p->T > 0)
+    for (const void* x : {fwd ? p->q : p->k, (const void*)(fwd ? p->o : p->v)}) {
+      if (!x) return S2ATTN_ERR_NULL;
+      if (!aligned(x, 16)) return S2ATTN_ERR_ALIGN;
+    }
+  if (fwd && !aligned(p->lse, 4)) return S2ATTN_ERR_ALIGN;
+  if (fwd && p->workspace && !aligned(p->workspace, kAlign)) return S2ATTN_ERR_ALIGN;
+  return S2ATTN_OK;
+}
+
+s2::PArgs make_args(const s2attn_paged_params* p, int H) {
+  s2::PArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.q = p->q; a.o = p->o; a.lse = p->lse; a.k = p->k; a.v = p->v;
+  a.kc = static_cast<char*>(p->k_cache); a.vc = static_cast<char*>(p->v_cache);
+  a.ke = p->k_exp; a.ve = p->v_exp;
+  a.table = p->page_table; a.row_start = p->row_start; a.kv_len = p->kv_len;
+  const long long cache_ext[3] = {p->pages, p->page_size, p->Hkv}, kv_ext[2] = {p->T, p->Hkv}, q_ext[2] = {p->T, H};
+  long long s2[2], s3[3];
+  resolve(p->q_strides, q_ext, p->D, s2); a.q_t = s2[0]; a.q_h = s2[1];
+  resolve(p->k_strides, kv_ext, p->D, s2); a.k_t = s2[0]; a.k_h = s2[1];
+  resolve(p->v_strides, kv_ext, p->D, s2); a.v_t = s2[0]; a.v_h = s2[1];
+  resolve(p->k_cache_strides, cache_ext, p->D, s3); a.kc_p = s3[0]; a.kc_t = s3[1]; a.kc_h = s3[2];
+  resolve(p->v_cache_strides, cache_ext, p->D, s3); a.vc_p = s3[0]; a.vc_t = s3[1]; a.vc_h = s3[2];
+  resolve(p->k_exp_strides, cache_ext, 1, s3); a.ke_p = s3[0]; a.ke_t = s3[1]; a.ke_h = s3[2];
+  resolve(p->v_exp_strides, cache_ext, 1, s3); a.ve_p = s3[0]; a.ve_t = s3[1]; a.ve_h = s3[2];
+  a.table_b = p->table_stride != 0 ? p->table_stride : p->table_cols;
+  a.T = p->T; a.B = p->B; a.Hkv = p->Hkv; a.r = H / p->Hkv;
+  a.pages = p->pages; a.page_size = p->page_size; a.max_keys = p->table_cols * p->page_size;
+  a.window = p->window >= kMost ? 0 : p->window;   // no position is that far from another
+  a.sinks = p->sinks;
+  a.splits = 1;
+  a.min_tiles = 1;
+  a.by_r = s2::div_by(a.r);
+  a.by_page = s2::div_by(a.page_size);
+  a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)p->D)) * 1.4426950408889634f;
+  return a;
+}
+
+int launched(int rc) { return rc == 0 ? S2ATTN_OK : S2ATTN_ERR_LAUNCH; }
+
+}  // namespace
+
+extern "C" {
+
+int s2attn_check_paged_args(const s2attn_paged_params* p, int call) { return check(p, call); }
+
+size_t s2attn_paged_workspace_bytes(const s2attn_paged_params* p) {
+  if (!p || !shape_valid(p) || p->H % p->Hkv != 0) return 0;
+  const Pieces x = pieces_wanted(p);
+  return x.splits > 1 ? x.splits * piece_bytes(p) : 0;
+}
+
+int s2attn_cache_write(const s2attn_paged_params* p, void* stream) {
+  int rc = check(p, S2ATTN_PAGED_WRITE);
+  if (rc == S2ATTN_OK) rc = s2::check_device();
+  if (rc != S2ATTN_OK || p->T == 0) return rc;
+  return launched(s2::launch_cache_write(make_args(p, p->Hkv), p->D, p->dtype, p->cache_dtype, static_cast<hipStream_t>(stream)));
+}
+
+int s2attn_cache_read(const s2attn_paged_params* p, void* stream) {
+  int rc = check(p, S2ATTN_PAGED_READ);
+  if (rc == S2ATTN_OK) rc = s2::check_device();
+  if (rc != S2ATTN_OK || p->T == 0) return rc;
+  return launched(s2::launch_cache_read(make_args(p, p->Hkv), p->D, p->dtype, p->cache_dtype, static_cast<hipStream_t>(stream)));
+}
+
+int s2attn_paged_fwd(const s2attn_paged_params* p, void* stream) {
+  int rc = check(p, S2ATTN_PAGED_FWD);
+  if (rc == S2ATTN_OK) rc = s2::check_device();
+  if (rc != S2ATTN_OK || p->T == 0) return rc;
+  s2::PArgs a = make_args(p, p->H);
+  const Pieces x = pieces_wanted(p);
+  a.n_tiles = (int)row_tiles(p);
+  const long long fit = p->workspace ? (long long)(p->workspace_bytes / piece_bytes(p)) : 0;
+  const long long blocks_fit = (INT_MAX - 8) / ((long long)a.n_tiles * a.Hkv);
+  a.splits = (int)std::max<long long>(1, std::min<long long>(x.splits, std::min(fit, blocks_fit)));
+  a.min_tiles = x.min_tiles;
+  if (a.splits > 1) {
+    a.part_o = static_cast<float*>(p->workspace);
+    a.part_lse = a.part_o + (size_t)a.splits * p->T * p->H * p->D;
+  }
+  a.by_tiles = s2::div_by(a.n_tiles);
+  a.by_groups = s2::div_by(a.Hkv * a.splits);
+  const int blocks = a.n_tiles * a.Hkv * a.splits;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool bf16 = p->dtype == S2ATTN_BF16;
+  rc = bf16 ? s2::launch_paged_bf16(a, p->D, p->cache_dtype, blocks, st) : s2::launch_paged_f32(a, p->D, p->cache_dtype, blocks, st);
+  if (rc == 0 && a.splits > 1) rc = s2::launch_paged_join(a, p->D, bf16, st);
+  return launched(rc);
+}
+
+}  // extern "C"

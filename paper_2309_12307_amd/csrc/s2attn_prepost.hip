@@ -108,6 +108,40 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* partial, void
   }
 }
 
+// dk, dv of the keys whose queries were cut into segments: the sum of all parts and segments, in order.  KT, QT: keys of a
+// key tile and queries of a query tile of the kernel that left them.
+template <bool BF16, int KT, int QT>
+__global__ void __launch_bounds__(256) sink_combine_kernel(KArgs a, Win win, Div by_row, Div by_keys) {
+  const int rows = win.sink_tiles * KT, i4 = block_id() * 256 + thread_id();
+  const int d4 = a.D / 4;
+  const int row = quot(i4, by_row), d = (i4 - row * d4) * 4;
+  const int bc = quot(row, by_keys), key = row - bc * rows;
+  const int b = bc / a.Hkv, c = bc - b * a.Hkv;
+  if (b >= a.B || key >= a.N) return;
+  const int jt = key / KT;
+  int segments = 1;
+  while (segments <= win.n_seg && query_tiles<KT, QT>(win, a.N, jt, segments).lo < query_tiles<KT, QT>(win, a.N, jt, segments).hi) ++segments;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int part = 0; part < a.parts; ++part)
+      for (int segment = 0; segment < segments; ++segment) {
+        const float4 x = *reinterpret_cast<const float4*>(far_row(win, a, which, part, segment, b, c, key, KT) + d);
+        r.x += x.x; r.y += x.y; r.z += x.z; r.w += x.w;
+      }
+    const size_t o = row_off(which == 0 ? a.sdk : a.sdv, b, key, c) + d;
+    void* out = which == 0 ? a.dk : a.dv;
+    if (BF16) {
+      uint2 pk;
+      pk.x = f32_to_bf16_bits(r.x) | (f32_to_bf16_bits(r.y) << 16);
+      pk.y = f32_to_bf16_bits(r.z) | (f32_to_bf16_bits(r.w) << 16);
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + o) = pk;
+    } else {
+      *reinterpret_cast<float4*>(static_cast<float*>(out) + o) = r;
+    }
+  }
+}
+
 }  // namespace
 
 template <int D, int HEADS>
@@ -122,6 +156,16 @@ static int launch_delta_t(const KArgs& a, hipStream_t st) {
 int launch_delta_bf16(const KArgs& a, hipStream_t st) {
   if (a.H % 2 != 0) return a.D == 64 ? launch_delta_t<64, 1>(a, st) : launch_delta_t<128, 1>(a, st);
   return a.D == 64 ? launch_delta_t<64, 2>(a, st) : launch_delta_t<128, 2>(a, st);
+}
+
+int launch_sink_combine(const KArgs& a, const Win& win, int dtype, hipStream_t st) {
+  const int rows = win.sink_tiles * (dtype == S2ATTN_BF16 ? 128 : 64), d4 = a.D / 4;
+  const dim3 grid((unsigned)(((long long)a.B * a.Hkv * rows * d4 + 255) / 256));
+  if (dtype == S2ATTN_BF16)
+    hipLaunchKernelGGL((sink_combine_kernel<true, 128, 64>), grid, dim3(256), 0, st, a, win, div_by(d4), div_by(rows));
+  else
+    hipLaunchKernelGGL((sink_combine_kernel<false, 64, 32>), grid, dim3(256), 0, st, a, win, div_by(d4), div_by(rows));
+  return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st) {
