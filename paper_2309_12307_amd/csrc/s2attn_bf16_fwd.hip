@@ -15,128 +15,12 @@
 // stages, one barrier per tile.  The output tile is transposed through LDS and stored
 // with 16-byte coalesced writes at the un-rolled token rows.
 #include "s2attn_bf16_common.h"
+#include "s2attn_bf16_fwd.h"
 #include "s2attn_device.h"
 #include "s2attn_launch.h"
 
 namespace s2 {
 namespace {
-
-constexpr int BN = 64;                       // keys per tile
-constexpr int kTileBytes = BN * kRowBytes;   // 16 KB
-constexpr float kRescaleThreshold = 8.f;     // log2 units
-
-struct FwdState {
-  f32x16 o_acc[4];
-  float m_run;    // running row maximum (raw score units), shared by lanes l and l^32
-  float l_run;    // this lane's part of the running row sum
-};
-
-// O^T += V^T P^T for the 16 keys starting at tile row KROW0.
-template <int KROW0>
-__device__ __forceinline__ void pv_step(FwdState& st, const char* Vs, const LaneOffsets& lo, bf16x8 pf) {
-  bf16x8 vf[4];
-#pragma unroll
-  for (int db = 0; db < 4; ++db) vf[db] = frag_tr<KROW0>(Vs, lo, db);
-#pragma unroll
-  for (int db = 0; db < 4; ++db) st.o_acc[db] = mfma32(vf[db], pf, st.o_acc[db]);
-}
-
-// S^T = K Q^T of one 64-key tile for one wave (32 queries): two 32-key blocks.
-// `masked` is wave-uniform: the tile touches the diagonal of this wave's rows.
-__device__ __forceinline__ void fwd_scores(f32x16& s0, f32x16& s1, const bf16x8 (&qf)[8], const char* Ks,
-                                           const LaneOffsets& lo, int j0, int qrow, int g32, bool masked) {
-  s0 = zero16();
-  s1 = zero16();
-  bf16x8 ka[4], kb[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    ka[i] = frag_rm<0>(Ks, lo, i);
-    kb[i] = frag_rm<32>(Ks, lo, i);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    s0 = mfma32(ka[i], qf[i], s0);
-    s1 = mfma32(kb[i], qf[i], s1);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    ka[i] = frag_rm<0>(Ks, lo, i + 4);
-    kb[i] = frag_rm<32>(Ks, lo, i + 4);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    s0 = mfma32(ka[i], qf[i + 4], s0);
-    s1 = mfma32(kb[i], qf[i + 4], s1);
-  }
-  if (masked) {
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int key = j0 + 8 * (v >> 2) + 4 * g32 + (v & 3);
-      if (key > qrow) s0[v] = -INFINITY;
-      if (key + 32 > qrow) s1[v] = -INFINITY;
-    }
-  }
-}
-
-// Online softmax of the tile: updates the running maximum lazily, accumulates the row
-// sum and packs the probabilities as the four 16-key B operands of the PV product.
-// The maximum of every tile is formed, sixteen instructions and a chain of ten.  Without it (a score far above the
-// running maximum shows in the row sum, and only then is the maximum formed and the exponentials taken again) N(0, 1)
-// inputs take 0.98 to 1.00 of the time, but others more, or P is rounded where it is not now: a row's largest P is 1 and
-// exact if the maximum was raised for it.  With the line at a sum of 2^8, as here, scores of standard deviation 3
-// take 1.04 of the time, of 8 1.12 (N = 8192, H = 32, G = 2048); at 2^12 of 8 1.05, and O is 5 % further from 64 bits at 16; at
-// 2^32 none takes longer, and dq leaves its bound.
-__device__ __forceinline__ void fwd_softmax(FwdState& st, f32x16& s0, f32x16& s1, float c2, bf16x8 (&pf)[4]) {
-  // two independent three-input maximum chains
-  float ma = fmaxf(s0[0], s0[1]), mb = fmaxf(s1[0], s1[1]);
-#pragma unroll
-  for (int v = 2; v < 16; v += 2) {
-    ma = fmaxf(fmaxf(ma, s0[v]), s0[v + 1]);
-    mb = fmaxf(fmaxf(mb, s1[v]), s1[v + 1]);
-  }
-  const float mx = max_halves(fmaxf(ma, mb));
-  if (__builtin_amdgcn_ballot_w64(mx * c2 > st.m_run * c2 + kRescaleThreshold) != 0) {
-    const float m_new = fmaxf(st.m_run, mx);
-    const float alpha = __builtin_amdgcn_exp2f((st.m_run - m_new) * c2);
-    st.m_run = m_new;
-    st.l_run *= alpha;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) st.o_acc[db][v] *= alpha;
-  }
-  const float mc = st.m_run * c2;
-  float ra = 0.f, rb = 0.f;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    s0[v] = __builtin_amdgcn_exp2f(fmaf(s0[v], c2, -mc));
-    s1[v] = __builtin_amdgcn_exp2f(fmaf(s1[v], c2, -mc));
-    ra += s0[v];
-    rb += s1[v];
-  }
-  st.l_run += ra + rb;
-  pf[0] = pack8(s0[0], s0[1], s0[2], s0[3], s0[4], s0[5], s0[6], s0[7]);
-  pf[1] = pack8(s0[8], s0[9], s0[10], s0[11], s0[12], s0[13], s0[14], s0[15]);
-  pf[2] = pack8(s1[0], s1[1], s1[2], s1[3], s1[4], s1[5], s1[6], s1[7]);
-  pf[3] = pack8(s1[8], s1[9], s1[10], s1[11], s1[12], s1[13], s1[14], s1[15]);
-}
-
-// O^T += V^T P^T for the whole 64-key tile.
-__device__ __forceinline__ void fwd_pv(FwdState& st, const char* Vs, const LaneOffsets& lo, const bf16x8 (&pf)[4]) {
-  pv_step<0>(st, Vs, lo, pf[0]);
-  pv_step<16>(st, Vs, lo, pf[1]);
-  pv_step<32>(st, Vs, lo, pf[2]);
-  pv_step<48>(st, Vs, lo, pf[3]);
-}
-
-__device__ __forceinline__ void fwd_tile(FwdState& st, const bf16x8 (&qf)[8], const char* Ks, const char* Vs,
-                                         const LaneOffsets& lo, int j0, int qrow, float c2, int g32, bool masked) {
-  f32x16 s0, s1;
-  bf16x8 pf[4];
-  fwd_scores(s0, s1, qf, Ks, lo, j0, qrow, g32, masked);
-  fwd_softmax(st, s0, s1, c2, pf);
-  fwd_pv(st, Vs, lo, pf);
-}
 
 // Removes what query row `qrow` does not see under a window.
 __device__ __forceinline__ void mask_window(f32x16& s0, f32x16& s1, int j0, int qrow, const Win& win, int g32) {
@@ -329,38 +213,6 @@ window_fwd_bf16_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
   fwd_workgroup<true, true>(a, T, deal, first_block + block_id(), win, smem);
 }
 
-// ---- the matrix block of the eight-wave kernel as 8 steps of 4 MFMAs, each fed by 4
-// operand fragments.  Steps 0-3: O^T += V^T P^T for keys 16k .. 16k+15 of the current
-// tile; steps 4-7: S^T += K Q^T over d = 32(k-4) .. +31 of the next tile.
-template <int STEP>
-__device__ __forceinline__ void pp_load(bf16x8 (&buf)[4], const char* Vs_cur, const char* Ks_nxt, const LaneOffsets& lo) {
-  if constexpr (STEP < 4) {
-#pragma unroll
-    for (int db = 0; db < 4; ++db) buf[db] = frag_tr<16 * STEP>(Vs_cur, lo, db);
-  } else {
-    constexpr int J = STEP - 4;
-    buf[0] = frag_rm<0>(Ks_nxt, lo, 2 * J);
-    buf[1] = frag_rm<32>(Ks_nxt, lo, 2 * J);
-    buf[2] = frag_rm<0>(Ks_nxt, lo, 2 * J + 1);
-    buf[3] = frag_rm<32>(Ks_nxt, lo, 2 * J + 1);
-  }
-}
-
-template <int STEP>
-__device__ __forceinline__ void pp_mma(const bf16x8 (&buf)[4], FwdState& st, const bf16x8 (&pf)[4],
-                                       const bf16x8 (&qf)[8], f32x16& s0, f32x16& s1) {
-  if constexpr (STEP < 4) {
-#pragma unroll
-    for (int db = 0; db < 4; ++db) st.o_acc[db] = mfma32(buf[db], pf[STEP], st.o_acc[db]);
-  } else {
-    constexpr int J = STEP - 4;
-    s0 = mfma32(buf[0], qf[2 * J], s0);
-    s1 = mfma32(buf[1], qf[2 * J], s1);
-    s0 = mfma32(buf[2], qf[2 * J + 1], s0);
-    s1 = mfma32(buf[3], qf[2 * J + 1], s1);
-  }
-}
-
 __device__ __forceinline__ void mask_scores(f32x16& s0, f32x16& s1, int j0, int qrow, int g32) {
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
@@ -548,10 +400,86 @@ fwd_bf16_pp_kernel(KArgs a, int T, Deal deal) {
   fwd_epilogue<RAGGED>(a, st, smem + w * (32 * kRowBytes), b, h, run, s, qw0, c2, lane, l32, g32);
 }
 
+// Eight waves under a window: one run of all tokens, the key tiles of the sinks and of the window.
+__global__ void __launch_bounds__(512, 1)
+window_fwd_bf16_pp_kernel(KArgs a, int T, Deal deal, Win win) {
+  constexpr int BM = 256;
+  __shared__ __attribute__((aligned(1024))) char smem[3 * 2 * kTileBytes];   // [stage][K,V]
+  const int tid = thread_id(), lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g32 = lane >> 5, l32 = lane & 31;
+  int seq, rank;
+  if (!decode_block(block_id(), T, deal, seq, rank)) return;
+  const HeadPos at = head_of_seq(a, seq);
+  const int c = at.c, b = at.b, h = at.h;
+  const int i0 = uni((T - 1 - rank) * BM);
+  const Run run{0, a.N};
+  const int qw0 = i0 + w * 32, qrow = qw0 + l32;
+  const KeyTiles kt = key_tiles<BN>(win.window, win.sinks, i0, i0 + BM - 1, a.N);
+  const float c2 = a.scale_log2;
+
+  bf16x8 qf[8];
+  {
+    const bf16x8* src = reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + row_off(a.sq, b, min(qrow, a.N - 1), h));
+#pragma unroll
+    for (int st = 0; st < 8; ++st) qf[st] = src[2 * st + g32];
+  }
+  const int st_row = 4 * w + (lane >> 4);
+  const uint64_t k_row_bytes = (uint64_t)a.sk.t * 2, v_row_bytes = (uint64_t)a.sv.t * 2;
+  const uint32_t smem_base = lds_addr(smem);
+  const uint32_t st_chunk = (uint32_t)(((lane & 15) ^ swz(st_row)) << 4);
+  const uint32_t k_lane = (uint32_t)(st_row * k_row_bytes) + st_chunk;
+  const uint32_t v_lane = (uint32_t)(st_row * v_row_bytes) + st_chunk;
+  const uint64_t k_head = uni64(reinterpret_cast<uint64_t>(a.k) + row_off(a.sk, b, 0, c) * 2);
+  const uint64_t v_head = uni64(reinterpret_cast<uint64_t>(a.v) + row_off(a.sv, b, 0, c) * 2);
+  auto issue = [&](int n, int stage) __attribute__((always_inline)) {
+    const uint32_t row0 = kt.tile(n) * BN;
+    const uint32_t ks = smem_base + stage * 2 * kTileBytes + 4 * w * kRowBytes;
+    if ((int)row0 + BN > a.N) {   // rows past the end repeat the last row
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const uint64_t tok = min((int)row0 + 32 * p + st_row, a.N - 1);
+        dma16(reinterpret_cast<const char*>(k_head + tok * k_row_bytes + st_chunk), ks + 32 * p * kRowBytes);
+        dma16(reinterpret_cast<const char*>(v_head + tok * v_row_bytes + st_chunk), ks + 32 * p * kRowBytes + kTileBytes);
+      }
+      return;
+    }
+    const uint64_t kb = k_head + row0 * k_row_bytes, vb = v_head + row0 * v_row_bytes;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      dma16s(kb + p * 32 * k_row_bytes, k_lane, ks + 32 * p * kRowBytes);
+      dma16s(vb + p * 32 * v_row_bytes, v_lane, ks + 32 * p * kRowBytes + kTileBytes);
+    }
+  };
+  LaneOffsets lo;
+  init_lane_offsets(lo, lane);
+  FwdState st;
+  st.m_run = first_max(c2);
+  st.l_run = 0.f;
+#pragma unroll
+  for (int db = 0; db < 4; ++db) st.o_acc[db] = zero16();
+  pp_walk(st, qf, lo, smem, kt.total, w >> 2, c2, issue, [](int) {},
+          [&](int n) {   // not after the wave's rows, and not between the sinks and their windows
+            const int j0 = kt.tile(n) * BN;
+            return j0 <= qw0 + 31 && qw0 < a.N && (j0 + BN > qw0 - win.window + 1 || j0 < win.sinks);
+          },
+          [&](f32x16& s0, f32x16& s1, int n) {
+            const int j0 = kt.tile(n) * BN;
+            if (j0 + BN - 1 > qw0 || j0 < qw0 + 31 - win.window + 1) mask_window(s0, s1, j0, qrow, win, g32);
+          });
+  __syncthreads();
+  fwd_epilogue<true>(a, st, smem + w * (32 * kRowBytes), b, h, run, 0, qw0, c2, lane, l32, g32);
+}
+
 }  // namespace
 
 int launch_window_fwd_bf16(const KArgs& a, const Win& win, hipStream_t st) {
   if (a.D == 64) return launch_window_fwd_d64(a, win, st);
+  if (win.window >= 1024) {
+    const int T = ragged_tiles(a, 256);
+    const Grid g = grid_of(T, a.B * a.H, a.r, 32);
+    hipLaunchKernelGGL(window_fwd_bf16_pp_kernel, dim3(g.blocks), dim3(512), 0, st, a, T, g.deal, win);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+  }
   const int T = ragged_tiles(a, 128);
   const Grid g = grid_of(T, a.B * a.H, a.r, 64);
   return launch_blocks(window_fwd_bf16_kernel, g.blocks, 256, st, a, T, g.deal, win);

@@ -6,6 +6,24 @@
 
 namespace s2 {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Sixteen e4m3 values times 2^(exps - 127) as bf16: exact, the products have four significant bits.
+__device__ __forceinline__ void widen(const uint4& u, float scale, bf16x8& lo, bf16x8& hi) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  bf16x2 p[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false);
+    p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lo[2 * i] = p[i][0]; lo[2 * i + 1] = p[i][1];
+    hi[2 * i] = p[4 + i][0]; hi[2 * i + 1] = p[4 + i][1];
+  }
+}
+
 template <int D>
 struct Tile;
 template <>

@@ -53,9 +53,10 @@ int check_device();
 struct PArgs;
 int launch_cache_write(const PArgs& a, int D, int dtype, int cache, hipStream_t st);
 int launch_cache_read(const PArgs& a, int D, int dtype, int cache, hipStream_t st);
-int launch_paged_bf16(const PArgs& a, int D, int cache, int blocks, hipStream_t st);
-int launch_paged_f32(const PArgs& a, int D, int cache, int blocks, hipStream_t st);
-int launch_paged_join(const PArgs& a, int D, bool bf16, hipStream_t st);   // splits > 1: after one of the two
+// nq: row blocks of 16 of the sequences of few rows
+int launch_paged_bf16(const PArgs& a, int D, bool e4m3, int nq, hipStream_t st);
+int launch_paged_f32(const PArgs& a, int D, bool e4m3, hipStream_t st);
+int launch_paged_join(const PArgs& a, int D, bool bf16, int nq, hipStream_t st);   // splits > 1: after one of the two
 
 // Number of tile sequences walked together (see decode_block) for a kernel whose XCD holds
 // `slots` workgroups at a time, and the sequence count padded to a multiple of it.

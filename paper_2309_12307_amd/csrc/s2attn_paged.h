@@ -8,6 +8,13 @@
 
 namespace s2 {
 
+// How the work of a launch, or of a part of it, is dealt out.
+struct PSet {
+  int splits, min_tiles;                       // most pieces the keys of a row tile are cut into; fewest key tiles of one
+  int n_tiles;                                 // row tiles (chunk), sequences (few)
+  Div by_tiles, by_groups, by_splits, by_min;  // n_tiles, Hkv * splits, splits, min_tiles
+};
+
 struct PArgs {
   const void* q; void* o; float* lse;          // (T,H,D), (T,H,D), (H,T) or null
   void* k; void* v;                            // rows of the call, (T,Hkv,D): written to the cache or read from it
@@ -21,9 +28,10 @@ struct PArgs {
   long long table_b;
   int T, B, H, Hkv, r, pages, page_size, max_keys;   // max_keys: table_cols * page_size
   int window, sinks;                           // window 0: every earlier key is visible
-  int splits, min_tiles;                       // most pieces the keys of a row tile are cut into; fewest key tiles of one
-  int n_tiles;                                 // row tiles of the launch (tile_of_block)
-  Div by_r, by_page, by_tiles, by_groups;
+  PSet chunk, few;                             // sequences of more than few_rows (row, head of the kv head) pairs, and the others
+  int few_rows, chunk_rows;                    // chunk_rows: of a row tile of `chunk`
+  int chunk_blocks;                            // blocks of `chunk`; those of `few` follow
+  Div by_r, by_page, by_Hkv;
   float scale_log2;
 };
 
@@ -68,26 +76,37 @@ __device__ __forceinline__ int find_seq(const PArgs& a, int id, int lane) {
 
 // Block -> (row tile, kv head, split).  Blocks of one (kv head, split) read the same keys: whole such groups go to an XCD
 // where they divide among the eight, row tiles from the last (most keys) to the first.
-__device__ __forceinline__ bool tile_of_block(const PArgs& a, int block, int& tile, int& c, int& split) {
-  const int groups = a.Hkv * a.splits;
+__device__ __forceinline__ bool tile_of_block(const PArgs& a, const PSet& set, int block, int& tile, int& c, int& split) {
+  const int groups = a.Hkv * set.splits;
   int g;
   if ((groups & 7) == 0) {
-    const int slot = block >> 3, u = quot(slot, a.by_tiles);
+    const int slot = block >> 3, u = quot(slot, set.by_tiles);
     g = u * 8 + (block & 7);
-    tile = slot - u * a.n_tiles;
+    tile = slot - u * set.n_tiles;
   } else {
-    tile = quot(block, a.by_groups);
+    tile = quot(block, set.by_groups);
     g = block - tile * groups;
   }
-  tile = a.n_tiles - 1 - tile;
-  split = g / a.Hkv;
+  tile = set.n_tiles - 1 - tile;
+  split = quot(g, a.by_Hkv);
   c = g - split * a.Hkv;
   return tile >= 0 && g < groups;
 }
 
-// Key tiles of a piece, and the pieces that `total` tiles make: at most `splits`, none of fewer than min_tiles tiles
-// (but the last).
-__device__ __forceinline__ int tiles_of_split(const PArgs& a, int total) { return max((total + a.splits - 1) / a.splits, a.min_tiles); }
+// Pieces that the `total` key tiles of a row tile are cut into (at most `splits`, of min_tiles tiles or more in the mean), and
+// the tiles of one: even ones.
+struct Piece {
+  int count, per;
+};
+__device__ __forceinline__ Piece pieces_of(const PSet& set, int total) {
+  Piece x{1, total};
+  if (set.splits > 1) {
+    x.count = max(min(set.splits, quot(total, set.by_min)), 1);
+    x.per = (total + x.count - 1) / x.count;
+    x.count = x.per > 0 ? (total + x.per - 1) / x.per : 1;
+  }
+  return x;
+}
 
 // The cache row of key position j: page number (-1: none) and place in the page.
 struct CacheRow {

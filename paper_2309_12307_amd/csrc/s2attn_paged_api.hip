@@ -61,29 +61,53 @@ bool shape_valid(const s2attn_paged_params* p) {
   return p->T >= 0 && p->B > 0 && p->H > 0 && p->Hkv > 0 && p->D > 0 && p->pages > 0 && p->page_size > 0 && p->table_cols > 0;
 }
 
-// Rows of a row tile of the attention kernels, as a power of two, and keys of a key tile.
-int tile_log2(const s2attn_paged_params* p) { return p->dtype == S2ATTN_F32 ? 6 : 7; }
 int tile_keys(const s2attn_paged_params* p) { return p->dtype == S2ATTN_F32 ? 32 : 64; }
 
-long long row_tiles(const s2attn_paged_params* p) { return (((long long)p->T * (p->H / p->Hkv)) >> tile_log2(p)) + p->B; }
+long long row_tiles(const s2attn_paged_params* p, int rows) { return (long long)p->T * (p->H / p->Hkv) / rows + p->B; }
 
-// How the keys of a row tile are dealt out: at most `splits` pieces of min_tiles key tiles or more.
-struct Pieces {
-  int splits, min_tiles;
+// Which sequences go to which kind of workgroup, and into how many pieces their keys are cut at most.
+struct Plan {
+  bool chunk, few;
+  int chunk_rows;              // of a row tile of `chunk`
+  int nq, few_rows;            // 16-row blocks of a `few` workgroup; the most rows of a sequence that goes there
+  int chunk_splits, chunk_min; // pieces, key tiles of a piece at least
+  int few_splits, few_min;
 };
-Pieces pieces_wanted(const s2attn_paged_params* p) {
-  const int TK = tile_keys(p);
+Plan plan(const s2attn_paged_params* p) {
+  Plan x{};
+  const long long r = p->H / p->Hkv, rows = p->T * r, seqs = std::max(1, std::min(p->B, p->T));
+  // One token a sequence (as far as T and B tell): all go to `few`, which takes any number of rows, by turns.  Where some have
+  // more, those of up to 32 rows go there and the others to `chunk`.
+  // (fp32: all to one of the two.)
+  const bool f32 = p->dtype == S2ATTN_F32;
+  x.nq = 1;
+  if ((p->T <= p->B && r <= 32) || rows <= 32) {
+    x.few = true;
+    if (!f32 && (p->T <= p->B ? r : rows) > 16) x.nq = 2;
+    x.few_rows = INT_MAX;
+  } else {
+    x.chunk = true;
+    x.few = !f32 && p->B > 1;
+    x.nq = 2;
+    x.few_rows = x.few ? 32 : 0;
+  }
   const long long most = (long long)p->table_cols * p->page_size;
-  const long long rows = (long long)p->T * (p->H / p->Hkv), seqs = std::max(1, std::min(p->B, p->T));
-  const long long tile = 1LL << tile_log2(p), in_tile = std::min(tile, (rows + seqs - 1) / seqs);
-  const long long blocks = std::max<long long>(1, std::max((rows + tile - 1) / tile, seqs) * p->Hkv);
   long long keys = p->max_kv > 0 ? std::min<long long>(p->max_kv, most) : most;
-  if (p->window > 0) keys = std::min<long long>(keys, (long long)p->window + p->sinks + (rows + seqs - 1) / seqs + 2 * TK);
-  const long long min_keys = std::max<long long>(256, 32 * in_tile);
-  const long long target = in_tile <= 16 ? 4096 : 512;
-  long long splits = std::min((keys + min_keys - 1) / min_keys, (target + blocks - 1) / blocks);
-  splits = std::max<long long>(1, std::min<long long>(splits, 256));
-  return Pieces{(int)splits, (int)(min_keys / TK)};
+  if (p->window > 0) keys = std::min<long long>(keys, (long long)p->window + p->sinks + (rows + seqs - 1) / seqs + 128);
+  auto pieces = [&](long long blocks, long long target, long long min_keys) {
+    const long long n = std::min((keys + min_keys - 1) / min_keys, (target + blocks - 1) / blocks);
+    return (int)std::max<long long>(1, std::min<long long>(n, 256));
+  };
+  // Eight waves on 256 rows where the sequences are long and their tiles fill the chip.
+  x.chunk_rows = f32 ? 64 : p->D == 128 && rows / seqs >= 512 && rows / 256 * p->Hkv >= 256 ? 256 : 128;
+  const long long tile = x.chunk_rows, in_tile = std::min(tile, (rows + seqs - 1) / seqs);
+  const long long tiles = std::max((rows + tile - 1) / tile, seqs);
+  const long long min_keys = std::max<long long>(256, 8 * in_tile);
+  x.chunk_splits = x.chunk ? pieces(tiles * p->Hkv, x.chunk_rows == 256 ? 256 : in_tile <= 16 ? 2048 : 512, min_keys) : 1;
+  x.chunk_min = (int)(min_keys / tile_keys(p));
+  x.few_splits = x.few ? pieces(seqs * p->Hkv, 2048, 256) : 1;
+  x.few_min = 256 / (f32 ? 16 : 32);
+  return x;
 }
 
 size_t piece_bytes(const s2attn_paged_params* p) { return (size_t)p->T * p->H * (p->D + 1) * sizeof(float); }
@@ -103,7 +127,7 @@ int check(const s2attn_paged_params* p, int call) {
   // positions, (row, head) pairs and block numbers are non-negative ints; a wave's pieces of a row are counted in them too
   if ((long long)p->table_cols * p->page_size > kMost || (long long)p->T * H > kMost || p->Hkv > 65536) return S2ATTN_ERR_TOO_LARGE;
   if ((long long)p->T * p->Hkv > kMost / 8 || p->B > (1 << 24)) return S2ATTN_ERR_TOO_LARGE;
-  if (fwd && row_tiles(p) * p->Hkv > kMost) return S2ATTN_ERR_TOO_LARGE;
+  if (fwd && row_tiles(p, 64) * p->Hkv > kMost / 2) return S2ATTN_ERR_TOO_LARGE;
 
   const int row_align = 16 / bytes_of(p->dtype), cache_align = 16 / bytes_of(p->cache_dtype);
   const long long cache_ext[3] = {p->pages, p->page_size, p->Hkv}, kv_ext[2] = {p->T, p->Hkv}, q_ext[2] = {p->T, H};
@@ -156,8 +180,7 @@ s2::PArgs make_args(const s2attn_paged_params* p, int H) {
   a.pages = p->pages; a.page_size = p->page_size; a.max_keys = p->table_cols * p->page_size;
   a.window = p->window >= kMost ? 0 : p->window;   // no position is that far from another
   a.sinks = p->sinks;
-  a.splits = 1;
-  a.min_tiles = 1;
+  a.by_Hkv = s2::div_by(p->Hkv);
   a.by_r = s2::div_by(a.r);
   a.by_page = s2::div_by(a.page_size);
   a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)p->D)) * 1.4426950408889634f;
@@ -174,8 +197,9 @@ int s2attn_check_paged_args(const s2attn_paged_params* p, int call) { return che
 
 size_t s2attn_paged_workspace_bytes(const s2attn_paged_params* p) {
   if (!p || !shape_valid(p) || p->H % p->Hkv != 0) return 0;
-  const Pieces x = pieces_wanted(p);
-  return x.splits > 1 ? x.splits * piece_bytes(p) : 0;
+  const Plan x = plan(p);
+  const int splits = std::max(x.chunk_splits, x.few_splits);
+  return splits > 1 ? splits * piece_bytes(p) : 0;
 }
 
 int s2attn_cache_write(const s2attn_paged_params* p, void* stream) {
@@ -197,23 +221,33 @@ int s2attn_paged_fwd(const s2attn_paged_params* p, void* stream) {
   if (rc == S2ATTN_OK) rc = s2::check_device();
   if (rc != S2ATTN_OK || p->T == 0) return rc;
   s2::PArgs a = make_args(p, p->H);
-  const Pieces x = pieces_wanted(p);
-  a.n_tiles = (int)row_tiles(p);
+  const Plan x = plan(p);
   const long long fit = p->workspace ? (long long)(p->workspace_bytes / piece_bytes(p)) : 0;
-  const long long blocks_fit = (INT_MAX - 8) / ((long long)a.n_tiles * a.Hkv);
-  a.splits = (int)std::max<long long>(1, std::min<long long>(x.splits, std::min(fit, blocks_fit)));
-  a.min_tiles = x.min_tiles;
-  if (a.splits > 1) {
+  auto set = [&](s2::PSet& s, int n_tiles, int splits, int min_tiles) {
+    const long long grid = (kMost / 2) / std::max(1LL, (long long)n_tiles * p->Hkv);
+    s.splits = (int)std::max<long long>(1, std::min<long long>(splits, std::min(fit, grid)));
+    s.min_tiles = min_tiles;
+    s.n_tiles = n_tiles;
+    s.by_tiles = s2::div_by(n_tiles);
+    s.by_groups = s2::div_by(p->Hkv * s.splits);
+    s.by_splits = s2::div_by(s.splits);
+    s.by_min = s2::div_by(min_tiles);
+    return n_tiles * p->Hkv * s.splits;
+  };
+  a.few_rows = x.few_rows;
+  a.chunk_rows = x.chunk_rows;
+  a.chunk_blocks = set(a.chunk, (int)row_tiles(p, x.chunk_rows), x.chunk_splits, x.chunk_min);
+  if (!x.chunk) a.chunk_blocks = 0;
+  set(a.few, p->B, x.few_splits, x.few_min);
+  const int splits = std::max(a.chunk.splits, a.few.splits);
+  if (splits > 1) {
     a.part_o = static_cast<float*>(p->workspace);
-    a.part_lse = a.part_o + (size_t)a.splits * p->T * p->H * p->D;
+    a.part_lse = a.part_o + (size_t)splits * p->T * p->H * p->D;
   }
-  a.by_tiles = s2::div_by(a.n_tiles);
-  a.by_groups = s2::div_by(a.Hkv * a.splits);
-  const int blocks = a.n_tiles * a.Hkv * a.splits;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool bf16 = p->dtype == S2ATTN_BF16;
-  rc = bf16 ? s2::launch_paged_bf16(a, p->D, p->cache_dtype, blocks, st) : s2::launch_paged_f32(a, p->D, p->cache_dtype, blocks, st);
-  if (rc == 0 && a.splits > 1) rc = s2::launch_paged_join(a, p->D, bf16, st);
+  const bool bf16 = p->dtype == S2ATTN_BF16, e4m3 = p->cache_dtype == S2ATTN_E4M3;
+  rc = bf16 ? s2::launch_paged_bf16(a, p->D, e4m3, x.nq, st) : s2::launch_paged_f32(a, p->D, e4m3, st);
+  if (rc == 0 && splits > 1) rc = s2::launch_paged_join(a, p->D, bf16, x.nq, st);
   return launched(rc);
 }
 

@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
   int tile, c, split;
-  if (!tile_of_block(a, first_block + block_id(), tile, c, split)) return;
+  if (!tile_of_block(a, a.chunk, first_block + block_id(), tile, c, split)) return;
   const int b = find_seq<kRowsLog2>(a, tile, lane);
   if (b < 0) return;
   const SeqRows sr = seq_rows(a, b);
@@ -33,8 +33,8 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   const int p_lo = uni(p_first + quot(i0, a.by_r));
   const int p_hi = uni(p_first + quot(min(i0 + kWgRows, n_rows) - 1, a.by_r));
   const KeyTiles kt = key_tiles<kTile>(a.window, a.sinks, p_lo, p_hi, sr.keys);
-  const int per = tiles_of_split(a, kt.total);
-  const int n0 = split * per, n1 = uni(min(kt.total, n0 + per));
+  const Piece piece = pieces_of(a.chunk, kt.total);
+  const int per = piece.per, n0 = split * per, n1 = uni(min(kt.total, n0 + per));
   if (split > 0 && n0 >= n1) return;
 
   const int iw = i0 + 16 * w, row = min(iw + c16, n_rows - 1);
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
   const float lse2 = l_tot == 0.f ? -INFINITY : m_run + log2f(l_tot);
   const int H = a.Hkv * a.r;
-  if (kt.total > per) {
+  if (piece.count > 1) {
     const size_t at = ((size_t)split * a.T + t) * H + h;
     store_row<D>(a.part_o + at * D, o, inv, q4);
     if (q4 == 0) a.part_lse[at] = lse2;
@@ -201,102 +201,328 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   if (q4 == 0 && a.lse) a.lse[(size_t)h * a.T + t] = lse2 * kLn2;
 }
 
-// o = sum of the pieces' outputs by their share exp2(lse_s - lse) of the row, one workgroup to a row: D / 4 lanes hold a
-// piece's output, so 8 or 16 pieces are in flight at a time, each group with a running maximum of its own.
-template <int D, int SHIFT, int TK, bool BF16>
-__global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, Div by_H, int first_block) {
-  constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+// ---- few rows: sixteen rows of a sequence, the waves on different tiles of 16 keys, K and V straight to registers, the next
+// tile on its way while one is worked on (as in the bf16 kernel; operands as in s2attn_f32_small.hip).
+//   K  lane (c16, q4) has key c16: fp32 floats 16 i + 4 q4 .., e4m3 values 16 (q4 + 4 i) ..; Q agrees
+//   V  lane (c16, q4) has keys 4 q4 + v, values 64 j + 4 c16 ..
+template <int D, bool E4M3>
+struct FewTile {
+  uint4 k[E4M3 ? D / 64 : D / 16];
+  uint32_t v8[4][D / 64];
+  f32x4 v[4][D / 64];
+  float ks, vs[4];
+  uint32_t seen;
+};
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int first_block) {
+  using T = FewTile<D, E4M3>;
+  constexpr int TK = 16, kWaves = 4, kEsz = E4M3 ? 1 : 4, kStride = D + 4;
+  __shared__ __attribute__((aligned(16))) float blocks[kWaves * 16 * kStride];
+  __shared__ float max_s[kWaves][16], sum_s[kWaves][16];
+  const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
+  const int c16 = lane & 15, q4 = lane >> 4;
+  const int block = first_block + block_id();
+  const int y = quot(block, a.by_Hkv), c = block - y * a.Hkv;
+  const int b = quot(y, a.few.by_splits), split = y - b * a.few.splits;
+  if (b >= a.B) return;
+  const SeqRows sr = seq_rows(a, b);
+  const int n_rows = uni(sr.n * a.r), p_first = uni(sr.kv - sr.n);
+  const char* k_head = a.kc + c * a.kc_h * kEsz + 16 * q4;
+  const char* v_head = a.vc + c * a.vc_h * kEsz + 4 * c16 * kEsz;
+  const float c2 = a.scale_log2;
+
+  for (int i0 = 0; i0 < n_rows; i0 += 16) {
+    const int p_lo = uni(p_first + quot(i0, a.by_r)), p_hi = uni(p_first + quot(min(i0 + 16, n_rows) - 1, a.by_r));
+    const KeyTiles kt = key_tiles<TK>(a.window, a.sinks, p_lo, p_hi, sr.keys);
+    const Piece piece = pieces_of(a.few, kt.total);
+    const int n0 = split * piece.per, n1 = uni(min(kt.total, n0 + piece.per));
+    if (split > 0 && n0 >= n1) continue;
+
+    auto look_up = [&](int n) __attribute__((always_inline)) {
+      return n < n1 ? cache_row(a, b, kt.tile(n) * TK + c16, kt.end) : CacheRow{-1, 0};
+    };
+    auto load = [&](T& t, const CacheRow& x) __attribute__((always_inline)) {
+      t.seen = (uint32_t)__builtin_amdgcn_ballot_w64(x.page >= 0) & 0xffffu;
+      const char* zero = reinterpret_cast<const char*>(zero_row);
+      const uint8_t* ze = reinterpret_cast<const uint8_t*>(zero);
+      const char* kp = x.page >= 0 ? k_head + (x.page * a.kc_p + x.at * a.kc_t) * kEsz : zero;
+#pragma unroll
+      for (int i = 0; i < (E4M3 ? D / 64 : D / 16); ++i) t.k[i] = *reinterpret_cast<const uint4*>(kp + 64 * i);
+      if constexpr (E4M3) t.ks = __uint_as_float((uint32_t)*(x.page >= 0 ? a.ke + x.page * a.ke_p + x.at * a.ke_t + c * a.ke_h : ze) << 23);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int page = __shfl(x.page, 4 * q4 + v), at = __shfl(x.at, 4 * q4 + v);
+        const char* vp = page >= 0 ? v_head + (page * a.vc_p + at * a.vc_t) * kEsz : zero;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+          if constexpr (E4M3) t.v8[v][j] = *reinterpret_cast<const uint32_t*>(vp + 64 * j);
+          else t.v[v][j] = *reinterpret_cast<const f32x4*>(vp + 256 * j);
+        }
+        if constexpr (E4M3) t.vs[v] = __uint_as_float((uint32_t)*(page >= 0 ? a.ve + page * a.ve_p + at * a.ve_t + c * a.ve_h : ze) << 23);
+      }
+    };
+    auto widen4 = [](uint32_t u, float s) __attribute__((always_inline)) {
+      const auto l = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), g = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+      return f32x4{l[0] * s, l[1] * s, g[0] * s, g[1] * s};
+    };
+
+    // the look-up of a tile goes out ahead of the loads of the tile before it, so that waiting for it is not waiting for them
+    T ta, tb;
+    CacheRow at = look_up(n0 + w), at_next = look_up(n0 + w + kWaves);
+    load(ta, at);
+    const int row = min(i0 + c16, n_rows - 1), tq = quot(row, a.by_r), h = c * a.r + row - tq * a.r;
+    const int p_row = p_first + tq, pos = min(p_row, sr.keys - 1), t = sr.s0 + tq;
+    f32x4 qf[D / 16];
+    {
+      const float* q = static_cast<const float*>(a.q) + t * a.q_t + h * a.q_h;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        qf[i] = *reinterpret_cast<const f32x4*>(q + (E4M3 ? 16 * (q4 + 4 * (i >> 2)) + 4 * (i & 3) : 16 * i + 4 * q4));
+    }
+    f32x4 o[D / 64][4];
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[j][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_run = -FLT_MAX, l_run = 0.f;
+
+    auto step = [&](T& cur, T& nxt, int n) __attribute__((always_inline)) {
+      at = at_next;
+      at_next = look_up(n + 2 * kWaves);
+      load(nxt, at);
+      const int j0 = kt.tile(n) * TK;
+      f32x4 sc = {0.f, 0.f, 0.f, 0.f}, odd = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        f32x4 x;
+        if constexpr (E4M3) {
+          const uint4 u = cur.k[i >> 2];
+          x = widen4((i & 3) == 0 ? u.x : (i & 3) == 1 ? u.y : (i & 3) == 2 ? u.z : u.w, cur.ks);
+        } else {
+          x = __builtin_bit_cast(f32x4, cur.k[i]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (i & 1) odd = mfma4(x[e], qf[i][e], odd);
+          else sc = mfma4(x[e], qf[i][e], sc);
+        }
+      }
+      sc += odd;
+      const bool windowed = a.window > 0 && j0 < p_hi - a.window + 1;
+      const bool masked = j0 + TK - 1 > p_lo || cur.seen != 0xffffu || windowed;
+      const int first = windowed ? p_row - a.window + 1 : 0;
+      const uint32_t seen_l = cur.seen >> (4 * q4);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        float x = sc[v] * c2;
+        const int key = j0 + 4 * q4 + v;
+        if (masked && !(key <= pos && (key >= first || key < a.sinks) && (seen_l >> v & 1))) x = -INFINITY;
+        sc[v] = x;
+        mx = fmaxf(mx, x);
+      }
+      mx = max_cols(mx);
+      if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+        const float m_new = fmaxf(m_run, mx);
+        const float alpha = exp2f(m_run - m_new);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[j][e] *= alpha;
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        sc[v] = exp2f(sc[v] - m_run);
+        l_run += sc[v];
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+          f32x4 x;
+          if constexpr (E4M3) x = widen4(cur.v8[v][j], cur.vs[v]);
+          else x = cur.v[v][j];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[j][e] = mfma4(x[e], sc[v], o[j][e]);
+        }
+    };
+    for (int n = n0 + w; n < n1; n += 2 * kWaves) {
+      step(ta, tb, n);
+      if (n + kWaves < n1) step(tb, ta, n + kWaves);
+    }
+
+    l_run = sum_cols(l_run);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<f32x4*>(blocks + (w * 16 + c16) * kStride + 64 * j + 16 * q4 + 4 * x) = f32x4{o[j][0][x], o[j][1][x], o[j][2][x], o[j][3][x]};
+    if (q4 == 0) {
+      max_s[w][c16] = m_run;
+      sum_s[w][c16] = l_run;
+    }
+    __syncthreads();
+    constexpr int kLanes = D / 8;   // 8 columns a thread: 16 or 32 rows at once
+    const int r16 = tid / kLanes, ch = tid % kLanes;
+    if (r16 < 16 && i0 + r16 < n_rows) {
+      float m = max_s[0][r16], l = 0.f;
+#pragma unroll
+      for (int x = 1; x < kWaves; ++x) m = fmaxf(m, max_s[x][r16]);
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+      for (int x = 0; x < kWaves; ++x) {
+        const float f = exp2f(max_s[x][r16] - m);
+        l = fmaf(sum_s[x][r16], f, l);
+        const f32x4* p = reinterpret_cast<const f32x4*>(blocks + (x * 16 + r16) * kStride + 8 * ch);
+        s0 += p[0] * f;
+        s1 += p[1] * f;
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+      const int ti = quot(i0 + r16, a.by_r), hi = c * a.r + i0 + r16 - ti * a.r, tt = sr.s0 + ti, H = a.Hkv * a.r;
+      float* dst;
+      if (piece.count > 1) {
+        const size_t at2 = ((size_t)split * a.T + tt) * H + hi;
+        dst = a.part_o + at2 * D;
+        if (ch == 0) a.part_lse[at2] = lse2;
+      } else {
+        dst = static_cast<float*>(a.o) + ((size_t)tt * H + hi) * D;
+        if (ch == 0 && a.lse) a.lse[(size_t)hi * a.T + tt] = lse2 * kLn2;
+      }
+      *reinterpret_cast<f32x4*>(dst + 8 * ch) = s0 * inv;
+      *reinterpret_cast<f32x4*>(dst + 8 * ch + 4) = s1 * inv;
+    }
+    __syncthreads();   // before the next rows' sums
+  }
+}
+
+// o = sum of the pieces' outputs by their share exp2(lse_s - lse) of the row.  D / 4 lanes hold a piece's output; of a workgroup's
+// groups of so many lanes G take the pieces of one row (each with a running maximum of its own), the others other heads of the
+// same token, `heads` of them to a workgroup.
+template <int D, int TK, int FEW_TK, bool BF16, int G>
+__global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, int nq, int heads, int head_blocks, Div by_head_blocks, int first_block) {
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAtOnce = kGroups / G;
   __shared__ float4 acc_s[kGroups][kLanes];
   __shared__ float m_s[kGroups], l_s[kGroups];
   const int tid = thread_id(), H = a.Hkv * a.r;
-  const int th = first_block + block_id(), t = quot(th, by_H), h = th - t * H;
+  const int block = first_block + block_id(), t = quot(block, by_head_blocks), h0 = (block - t * head_blocks) * heads;
   if (t >= a.T) return;
   const int b = find_seq<-1>(a, t, tid & 63);
   if (b < 0) return;
   const SeqRows sr = seq_rows(a, b);
   if (t >= sr.s0 + sr.n) return;
-  const int i = (t - sr.s0) * a.r + (h - quot(h, a.by_r) * a.r), i0 = i & ~((1 << SHIFT) - 1);
-  const int p_first = sr.kv - sr.n;
-  const KeyTiles kt = key_tiles<TK>(a.window, a.sinks, p_first + quot(i0, a.by_r),
-                                    p_first + quot(min(i0 + (1 << SHIFT), sr.n * a.r) - 1, a.by_r), sr.keys);
-  const int per = tiles_of_split(a, kt.total);
-  if (kt.total <= per) return;                    // in one piece: written by the attention kernel
-  const int pieces = (kt.total + per - 1) / per;
-
-  const int g = tid / kLanes, l = tid % kLanes;
+  const int n_rows = sr.n * a.r, p_first = sr.kv - sr.n;
+  const bool few = n_rows <= a.few_rows;
+  const int tile = few ? 16 * nq : a.chunk_rows;
+  const PSet& set = few ? a.few : a.chunk;
+  if (set.splits == 1) return;                    // in one piece: written by the attention kernel
+  const int g = tid / kLanes, l = tid % kLanes, sub = g / G, piece0 = g % G;
   const size_t step = (size_t)a.T * H;
-  const float* po = a.part_o + ((size_t)t * H + h) * D + 4 * l;
-  const float* pl = a.part_lse + (size_t)t * H + h;
-  float m = -FLT_MAX, sum = 0.f;
-  float4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = g; s0 < pieces; s0 += 4 * kGroups) {
-    float ls[4];
-    float4 x[4];
+  for (int hh = 0; hh < heads; hh += kAtOnce) {
+    const int h = h0 + hh + sub;
+    const bool on = hh + sub < heads && h < H;
+    const int i = (t - sr.s0) * a.r + (h - quot(h, a.by_r) * a.r), j0 = i & ~(tile - 1);   // tile: a power of two
+    const int p_lo = p_first + quot(j0, a.by_r), p_hi = p_first + quot(min(j0 + tile, n_rows) - 1, a.by_r);
+    const KeyTiles kt = few ? key_tiles<FEW_TK>(a.window, a.sinks, p_lo, p_hi, sr.keys) : key_tiles<TK>(a.window, a.sinks, p_lo, p_hi, sr.keys);
+    const Piece piece = pieces_of(set, kt.total);
+    const int pieces = on && piece.count > 1 ? piece.count : 0;
+    const float* po = a.part_o + ((size_t)t * H + h) * D + 4 * l;
+    const float* pl = a.part_lse + (size_t)t * H + h;
+    float m = -FLT_MAX, sum = 0.f;
+    float4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = piece0; s0 < pieces; s0 += 4 * G) {
+      float ls[4];
+      float4 x[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int s = s0 + u * kGroups;
-      ls[u] = s < pieces ? pl[s * step] : -INFINITY;
-      x[u] = s < pieces ? *reinterpret_cast<const float4*>(po + s * step * D) : float4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < 4; ++u) {
+        const int s = s0 + u * G;
+        ls[u] = s < pieces ? pl[s * step] : -INFINITY;
+        x[u] = s < pieces ? *reinterpret_cast<const float4*>(po + s * step * D) : float4{0.f, 0.f, 0.f, 0.f};
+      }
+      const float m_new = fmaxf(fmaxf(fmaxf(m, ls[0]), ls[1]), fmaxf(ls[2], ls[3]));
+      const float alpha = exp2f(m - m_new);
+      m = m_new;
+      sum *= alpha;
+      acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float f = exp2f(ls[u] - m);
+        sum += f;
+        acc.x = fmaf(x[u].x, f, acc.x); acc.y = fmaf(x[u].y, f, acc.y);
+        acc.z = fmaf(x[u].z, f, acc.z); acc.w = fmaf(x[u].w, f, acc.w);
+      }
     }
-    const float m_new = fmaxf(fmaxf(fmaxf(m, ls[0]), ls[1]), fmaxf(ls[2], ls[3]));
-    const float alpha = exp2f(m - m_new);
-    m = m_new;
-    sum *= alpha;
-    acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+    if constexpr (G > 1) {
+      acc_s[g][l] = acc;
+      if (l == 0) { m_s[g] = m; l_s[g] = sum; }
+      __syncthreads();
+      if (piece0 == 0) {
+        float top = m;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float f = exp2f(ls[u] - m);
-      sum += f;
-      acc.x = fmaf(x[u].x, f, acc.x); acc.y = fmaf(x[u].y, f, acc.y);
-      acc.z = fmaf(x[u].z, f, acc.z); acc.w = fmaf(x[u].w, f, acc.w);
+        for (int x = 1; x < G; ++x) top = fmaxf(top, m_s[g + x]);
+        sum = 0.f;
+        acc = float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < G; ++x) {
+          const float f = exp2f(m_s[g + x] - top);
+          sum = fmaf(l_s[g + x], f, sum);
+          acc.x = fmaf(acc_s[g + x][l].x, f, acc.x); acc.y = fmaf(acc_s[g + x][l].y, f, acc.y);
+          acc.z = fmaf(acc_s[g + x][l].z, f, acc.z); acc.w = fmaf(acc_s[g + x][l].w, f, acc.w);
+        }
+        m = top;
+      }
+      __syncthreads();   // before the next heads' sums
     }
+    if (piece0 != 0 || pieces == 0) continue;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t at = ((size_t)t * H + h) * D + 4 * l;
+    if constexpr (BF16)
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.o) + at) = pack4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    else
+      *reinterpret_cast<float4*>(static_cast<float*>(a.o) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    if (l == 0 && a.lse) a.lse[(size_t)h * a.T + t] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
   }
-  acc_s[g][l] = acc;
-  if (l == 0) { m_s[g] = m; l_s[g] = sum; }
-  __syncthreads();
-  if (g != 0) return;
-  float top = m_s[0];
-#pragma unroll
-  for (int x = 1; x < kGroups; ++x) top = fmaxf(top, m_s[x]);
-  float total = 0.f;
-  acc = float4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int x = 0; x < kGroups; ++x) {
-    const float f = exp2f(m_s[x] - top);
-    total = fmaf(l_s[x], f, total);
-    acc.x = fmaf(acc_s[x][l].x, f, acc.x); acc.y = fmaf(acc_s[x][l].y, f, acc.y);
-    acc.z = fmaf(acc_s[x][l].z, f, acc.z); acc.w = fmaf(acc_s[x][l].w, f, acc.w);
-  }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
-  const size_t at = ((size_t)t * H + h) * D + 4 * l;
-  if constexpr (BF16)
-    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.o) + at) = pack4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-  else
-    *reinterpret_cast<float4*>(static_cast<float*>(a.o) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-  if (l == 0 && a.lse) a.lse[(size_t)h * a.T + t] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
-template <int D>
-int launch_t(const PArgs& a, int cache, int blocks, hipStream_t st) {
-  if (cache == 2) return launch_blocks(paged_f32_kernel<D, true>, blocks, 256, st, a);
-  return launch_blocks(paged_f32_kernel<D, false>, blocks, 256, st, a);
+template <int D, int TK, int FEW_TK, bool BF16>
+int join_t(const PArgs& a, int nq, hipStream_t st) {
+  constexpr int kGroups = 1024 / D;
+  const int H = a.Hkv * a.r, splits = a.few.splits > a.chunk.splits ? a.few.splits : a.chunk.splits;
+  // four pieces in flight to a group; heads go together while 1024 workgroups are left
+  const int G = splits <= 4 ? 1 : splits <= 8 ? 2 : splits <= 16 ? 4 : 8;
+  int heads = kGroups / G;
+  while (2 * heads <= H && (long long)a.T * (H / (2 * heads)) >= 1024) heads *= 2;
+  const int head_blocks = (H + heads - 1) / heads;
+  const Div d = div_by(head_blocks);
+  const int blocks = a.T * head_blocks;
+  if (G == 1) return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 1>, blocks, 256, st, a, nq, heads, head_blocks, d);
+  if (G == 2) return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 2>, blocks, 256, st, a, nq, heads, head_blocks, d);
+  if (G == 4) return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 4>, blocks, 256, st, a, nq, heads, head_blocks, d);
+  return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 8>, blocks, 256, st, a, nq, heads, head_blocks, d);
 }
 
 }  // namespace
 
-int launch_paged_f32(const PArgs& a, int D, int cache, int blocks, hipStream_t st) {
-  return D == 64 ? launch_t<64>(a, cache, blocks, st) : launch_t<128>(a, cache, blocks, st);
+int launch_paged_f32(const PArgs& a, int D, bool e4m3, hipStream_t st) {
+  if (a.chunk_blocks == 0) {
+    const int few = a.B * a.Hkv * a.few.splits;
+    if (D == 64) return e4m3 ? launch_blocks(paged_few_f32_kernel<64, true>, few, 256, st, a)
+                             : launch_blocks(paged_few_f32_kernel<64, false>, few, 256, st, a);
+    return e4m3 ? launch_blocks(paged_few_f32_kernel<128, true>, few, 256, st, a)
+                : launch_blocks(paged_few_f32_kernel<128, false>, few, 256, st, a);
+  }
+  if (D == 64) return e4m3 ? launch_blocks(paged_f32_kernel<64, true>, a.chunk_blocks, 256, st, a)
+                           : launch_blocks(paged_f32_kernel<64, false>, a.chunk_blocks, 256, st, a);
+  return e4m3 ? launch_blocks(paged_f32_kernel<128, true>, a.chunk_blocks, 256, st, a)
+              : launch_blocks(paged_f32_kernel<128, false>, a.chunk_blocks, 256, st, a);
 }
 
-int launch_paged_join(const PArgs& a, int D, bool bf16, hipStream_t st) {
-  const int H = a.Hkv * a.r, rows = a.T * H;
-  const Div by_H = div_by(H);
-  if (bf16) {
-    if (D == 64) return launch_blocks(paged_join_kernel<64, 7, 64, true>, rows, 256, st, a, by_H);
-    return launch_blocks(paged_join_kernel<128, 7, 64, true>, rows, 256, st, a, by_H);
-  }
-  if (D == 64) return launch_blocks(paged_join_kernel<64, 6, 32, false>, rows, 256, st, a, by_H);
-  return launch_blocks(paged_join_kernel<128, 6, 32, false>, rows, 256, st, a, by_H);
+int launch_paged_join(const PArgs& a, int D, bool bf16, int nq, hipStream_t st) {
+  if (bf16) return D == 64 ? join_t<64, 64, 32, true>(a, nq, st) : join_t<128, 64, 32, true>(a, nq, st);
+  return D == 64 ? join_t<64, 32, 16, false>(a, nq, st) : join_t<128, 32, 16, false>(a, nq, st);
 }
 
 }  // namespace s2
