@@ -22,14 +22,18 @@
 namespace s2 {
 namespace {
 
-// Removes what query row `qrow` does not see under a window.
+// Removes what query row `qrow` does not see under a window: key <= qrow and qrow - key < window in one comparison.  One way
+// through and not two (tiles without sinks by themselves): the compiler then moves the scores to other registers.
 __device__ __forceinline__ void mask_window(f32x16& s0, f32x16& s1, int j0, int qrow, const Win& win, int g32) {
-  const int first = qrow - win.window + 1;
+  int d0 = qrow - j0 - 4 * g32;
+  asm volatile("" : "+v"(d0));   // keeps the compiler from doing all this ahead of the branch that asks for it
+  const unsigned n = win.window;
+  const int last = min(qrow, win.sinks - 1) - j0 - 4 * g32;   // keys up to it are sinks that the row sees
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
-    const int key = j0 + 8 * (v >> 2) + 4 * g32 + (v & 3);
-    if (key > qrow || (key < first && key >= win.sinks)) s0[v] = -INFINITY;
-    if (key + 32 > qrow || (key + 32 < first && key + 32 >= win.sinks)) s1[v] = -INFINITY;
+    const int bit = 8 * (v >> 2) + (v & 3);
+    s0[v] = (((unsigned)(d0 - bit) < n) | (bit <= last)) ? s0[v] : -INFINITY;
+    s1[v] = (((unsigned)(d0 - bit - 32) < n) | (bit + 32 <= last)) ? s1[v] : -INFINITY;
   }
 }
 
@@ -474,7 +478,10 @@ window_fwd_bf16_pp_kernel(KArgs a, int T, Deal deal, Win win) {
 
 int launch_window_fwd_bf16(const KArgs& a, const Win& win, hipStream_t st) {
   if (a.D == 64) return launch_window_fwd_d64(a, win, st);
-  if (win.window >= 1024) {
+  // Eight waves only for long walks: of the tiles that 256 rows meet a wave's 32 need all but three or four, and one workgroup a
+  // CU has nothing beside its first and last tile.  us, four waves and eight, N = 32768, H = 32, four sinks: window 1024 756
+  // and 786, 2048 1252 and 1260, 4096 2193 and 2089, 8192 3833 and 3564; N = 4096 2048 131 and 127, 4096 146 and 137.
+  if (win.window >= 4096) {
     const int T = ragged_tiles(a, 256);
     const Grid g = grid_of(T, a.B * a.H, a.r, 32);
     hipLaunchKernelGGL(window_fwd_bf16_pp_kernel, dim3(g.blocks), dim3(512), 0, st, a, T, g.deal, win);

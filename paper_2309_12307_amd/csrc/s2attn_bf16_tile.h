@@ -9,7 +9,8 @@ namespace s2 {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // Sixteen e4m3 values times 2^(exps - 127) as bf16: exact, the products have four significant bits.
-__device__ __forceinline__ void widen(const uint4& u, float scale, bf16x8& lo, bf16x8& hi) {
+template <class Vec>
+__device__ __forceinline__ void widen(const Vec& u, float scale, bf16x8& lo, bf16x8& hi) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
   bf16x2 p[8];
 #pragma unroll

@@ -21,7 +21,6 @@ enum { kBf16 = 0, kF32 = 1, kE4m3 = 2 };
 constexpr int kBytes[3] = {2, 4, 1};
 constexpr int kSteps = 4;   // pieces of a lane, in flight together
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
@@ -124,7 +123,7 @@ __device__ __forceinline__ Values<ROWS, 16> restore(const u32x4& u, float scale)
   Values<ROWS, 16> r;
   if constexpr (ROWS == kBf16) {
     bf16x8 lo, hi;
-    widen(__builtin_bit_cast(uint4, u), scale, lo, hi);
+    widen(u, scale, lo, hi);
     r.x[0] = __builtin_bit_cast(u32x4, lo);
     r.x[1] = __builtin_bit_cast(u32x4, hi);
   } else {

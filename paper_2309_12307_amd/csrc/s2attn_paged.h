@@ -30,6 +30,7 @@ struct PArgs {
   int window, sinks;                           // window 0: every earlier key is visible
   PSet chunk, few;                             // sequences of more than few_rows (row, head of the kv head) pairs, and the others
   int few_rows, chunk_rows;                    // chunk_rows: of a row tile of `chunk`
+  int by16;                                    // pages of a multiple of 16 tokens, 16 rows of one within 31-bit offsets
   int chunk_blocks;                            // blocks of `chunk`; those of `few` follow
   Div by_r, by_page, by_Hkv;
   float scale_log2;
@@ -123,7 +124,78 @@ __device__ __forceinline__ CacheRow cache_row(const PArgs& a, int b, int j, int 
   return x;
 }
 
-// A wave's 16 bytes that stand for a row that is not there.
+// Keys that a row sees up to `pos` without the sinks: all, or those of its window (pos is less than its position p_row where the
+// sequence is cut off).
+__device__ __forceinline__ int keys_up_to(int window, int p_row, int pos) {
+  return max(window > 0 ? pos - max(p_row - window, -1) : pos + 1, 0);
+}
+
+// Where pages are of a multiple of 16 tokens, 16 keys from a multiple of 16 on lie in one page, one after the other: one look-up
+// on the scalar unit and no address arithmetic a lane.  Page numbers of the N such groups of a tile.
+template <int N>
+struct Groups {
+  int page[N];
+};
+template <int N>
+__device__ __forceinline__ Groups<N> groups_of(const PArgs& a, int b, int j0) {
+  Groups<N> x;
+#pragma unroll
+  for (int g = 0; g < N; ++g) x.page[g] = a.table[b * a.table_b + quot(min(j0 + 16 * g, a.max_keys - 1), a.by_page)];
+  return x;
+}
+// The place in its page of key j0, and a bit for each key of the tile that exists.
+__device__ __forceinline__ int place_of(const PArgs& a, int j0) { return j0 - quot(j0, a.by_page) * a.page_size; }
+// Bytes from a cache's first row (of a head) to place `at` of page `page`, all factors below 2^32 where a.by16.
+__device__ __forceinline__ uint64_t group_off(int page, int at, long long page_bytes, long long token_bytes) {
+  return (uint64_t)(uint32_t)page * (uint32_t)page_bytes + (uint32_t)at * (uint32_t)token_bytes;
+}
+template <int N>
+__device__ __forceinline__ uint64_t seen_of(const PArgs& a, const Groups<N>& x, int j0, int end) {
+  uint64_t seen = 0;
+#pragma unroll
+  for (int g = 0; g < N; ++g)
+    if ((unsigned)x.page[g] < (unsigned)a.pages) seen |= 0xffffull << (16 * g);
+  const int left = end - j0;   // keys before `end`
+  return left >= 16 * N ? seen : left <= 0 ? 0 : seen & ((1ull << left) - 1);
+}
+
+// Tiles [from, n1) of TK keys of a walk lie on pages that exist and before `end`: their loads need no test.  The tiles of the sinks and
+// the first of the window stay out: pages between may have been given up.  The whole workgroup of THREADS looks.
+struct Plain {
+  int from, to;
+};
+template <int TK, int THREADS>
+__device__ __forceinline__ Plain plain_tiles(const PArgs& a, int b, const KeyTiles& kt, int n0, int n1, int tid, int* flags) {
+  Plain x;
+  x.from = a.window > 0 ? max(n0, kt.n_sink + 1) : n0;
+  x.to = min(n1, kt.n_sink + kt.end / TK - kt.first);   // (the last tile may reach past `end`)
+  bool bad = false;
+  if (x.from < x.to) {
+    const int first = quot(kt.tile(x.from) * TK, a.by_page), last = quot(kt.tile(x.to - 1) * TK + TK - 1, a.by_page);
+    const int* row = a.table + b * a.table_b;
+    for (int s = first + tid; s <= last; s += 4 * THREADS)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) bad |= (unsigned)row[min(s + u * THREADS, last)] >= (unsigned)a.pages;
+  }
+  const bool wave_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+  if ((tid & 63) == 0) flags[tid >> 6] = wave_bad;
+  __syncthreads();
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) any |= flags[w];
+  if (wave_uniform(any)) x.to = x.from;
+  return x;
+}
+
+// What stands for a row that is not there.
 static __device__ const uint4 zero_row[32] = {};
+
+// Loads from addresses that are global memory, said so: a choice between the cache and zero_row otherwise becomes a flat load,
+// which waits for LDS too.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#define S2_GLOBAL(T, p) (*(const __attribute__((address_space(1))) T*)(p))
+__device__ __forceinline__ uint64_t zero_address() { return reinterpret_cast<uint64_t>(&zero_row[0]); }
+__device__ __forceinline__ u32x4 load16(uint64_t p) { return S2_GLOBAL(u32x4, p); }
+__device__ __forceinline__ float load_scale(uint64_t p) { return __uint_as_float((uint32_t)S2_GLOBAL(uint8_t, p) << 23); }
 
 }  // namespace s2

@@ -73,7 +73,7 @@ struct Plan {
   int chunk_splits, chunk_min; // pieces, key tiles of a piece at least
   int few_splits, few_min;
 };
-Plan plan(const s2attn_paged_params* p) {
+Plan plan(const s2attn_paged_params* p, bool by16) {
   Plan x{};
   const long long r = p->H / p->Hkv, rows = p->T * r, seqs = std::max(1, std::min(p->B, p->T));
   // One token a sequence (as far as T and B tell): all go to `few`, which takes any number of rows, by turns.  Where some have
@@ -99,7 +99,7 @@ Plan plan(const s2attn_paged_params* p) {
     return (int)std::max<long long>(1, std::min<long long>(n, 256));
   };
   // Eight waves on 256 rows where the sequences are long and their tiles fill the chip.
-  x.chunk_rows = f32 ? 64 : p->D == 128 && rows / seqs >= 512 && rows / 256 * p->Hkv >= 256 ? 256 : 128;
+  x.chunk_rows = f32 ? 64 : by16 && p->D == 128 && rows / seqs >= 512 && rows / 256 * p->Hkv >= 256 ? 256 : 128;
   const long long tile = x.chunk_rows, in_tile = std::min(tile, (rows + seqs - 1) / seqs);
   const long long tiles = std::max((rows + tile - 1) / tile, seqs);
   const long long min_keys = std::max<long long>(256, 8 * in_tile);
@@ -159,6 +159,15 @@ int check(const s2attn_paged_params* p, int call) {
   return S2ATTN_OK;
 }
 
+// 16 keys of a group lie in one page, and offsets within a page, of pages and of the rows of a group fit the arithmetic on the
+// scalar unit.
+bool groups_of_16(const s2attn_paged_params* p, const s2::PArgs& a) {
+  if (p->page_size % 16 != 0) return false;
+  const long long esz = bytes_of(p->cache_dtype), page = std::max(a.kc_p, a.vc_p) * esz, token = std::max(a.kc_t, a.vc_t) * esz;
+  const long long exps = p->cache_dtype == S2ATTN_E4M3 ? std::max(a.ke_t, a.ve_t) : 0;
+  return std::max(token, exps) < (1LL << 31) / 16 && std::max(page, token * p->page_size) < (1LL << 32);
+}
+
 s2::PArgs make_args(const s2attn_paged_params* p, int H) {
   s2::PArgs a;
   std::memset(&a, 0, sizeof(a));
@@ -181,6 +190,7 @@ s2::PArgs make_args(const s2attn_paged_params* p, int H) {
   a.window = p->window >= kMost ? 0 : p->window;   // no position is that far from another
   a.sinks = p->sinks;
   a.by_Hkv = s2::div_by(p->Hkv);
+  a.by16 = groups_of_16(p, a);
   a.by_r = s2::div_by(a.r);
   a.by_page = s2::div_by(a.page_size);
   a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)p->D)) * 1.4426950408889634f;
@@ -197,7 +207,7 @@ int s2attn_check_paged_args(const s2attn_paged_params* p, int call) { return che
 
 size_t s2attn_paged_workspace_bytes(const s2attn_paged_params* p) {
   if (!p || !shape_valid(p) || p->H % p->Hkv != 0) return 0;
-  const Plan x = plan(p);
+  const Plan x = plan(p, make_args(p, p->H).by16);
   const int splits = std::max(x.chunk_splits, x.few_splits);
   return splits > 1 ? splits * piece_bytes(p) : 0;
 }
@@ -221,7 +231,7 @@ int s2attn_paged_fwd(const s2attn_paged_params* p, void* stream) {
   if (rc == S2ATTN_OK) rc = s2::check_device();
   if (rc != S2ATTN_OK || p->T == 0) return rc;
   s2::PArgs a = make_args(p, p->H);
-  const Plan x = plan(p);
+  const Plan x = plan(p, a.by16);
   const long long fit = p->workspace ? (long long)(p->workspace_bytes / piece_bytes(p)) : 0;
   auto set = [&](s2::PSet& s, int n_tiles, int splits, int min_tiles) {
     const long long grid = (kMost / 2) / std::max(1LL, (long long)n_tiles * p->Hkv);

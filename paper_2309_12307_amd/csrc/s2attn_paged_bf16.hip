@@ -12,6 +12,8 @@
 //
 // P is rounded to bf16 for the second product (as everywhere in this library); the row sum adds the unrounded P, and
 // statistics, outputs and partial outputs stay fp32 up to the one rounding of o.
+#include <type_traits>
+
 #include "s2attn_bf16_fwd.h"
 #include "s2attn_bf16_tile.h"
 #include "s2attn_launch.h"
@@ -24,15 +26,18 @@ constexpr int kKeys = 64;       // of a tile
 constexpr int kRowsLog2 = 7;
 constexpr int kRows = 1 << kRowsLog2;
 
-// Removes the scores of keys that this lane's row does not see: after `pos`, before `first` and no sinks, or not there (`seen`: a
-// bit a key, from this lane's first on, which is `key0`).
-__device__ __forceinline__ void mask_paged(f32x16& s0, f32x16& s1, int key0, int pos, int first, int sinks, uint64_t seen) {
+// Removes the scores of keys that this lane's row does not see: those but the `n` up to `pos` and the sinks up to it, and those on
+// pages that do not exist.  `key0`: this lane's first key; `seen`: a bit a key from there on.
+__device__ __forceinline__ void mask_paged(f32x16& s0, f32x16& s1, int key0, int pos, int n, int sinks, uint64_t seen) {
+  int d0 = pos - key0;
+  asm volatile("" : "+v"(d0));   // keeps the compiler from doing all this ahead of the branch that asks for it
+  const int last = min(pos, sinks - 1) - key0;   // keys up to it are sinks that the row sees
   const uint32_t seen0 = (uint32_t)seen, seen1 = (uint32_t)(seen >> 32);
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
-    const int bit = 8 * (v >> 2) + (v & 3), key = key0 + bit;
-    if (!(key <= pos && (key >= first || key < sinks) && (seen0 >> bit & 1))) s0[v] = -INFINITY;
-    if (!(key + 32 <= pos && (key + 32 >= first || key + 32 < sinks) && (seen1 >> bit & 1))) s1[v] = -INFINITY;
+    const int bit = 8 * (v >> 2) + (v & 3);
+    s0[v] = ((((unsigned)(d0 - bit) < (unsigned)n) | (bit <= last)) & (seen0 >> bit & 1)) ? s0[v] : -INFINITY;
+    s1[v] = ((((unsigned)(d0 - bit - 32) < (unsigned)n) | (bit + 32 <= last)) & (seen1 >> bit & 1)) ? s1[v] : -INFINITY;
   }
 }
 
@@ -85,8 +90,8 @@ __device__ __forceinline__ void chunk_epilogue(const PArgs& a, const f32x16 (&o)
 }
 
 // smem: [stage][K, V]
-template <int D, bool E4M3>
-__device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char* smem) {
+template <int D, bool E4M3, bool BY16>
+__device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char* smem, int* flags) {
   using L = Tile<D>;
   constexpr int kTileBytes = kKeys * L::kRow;
   constexpr int KS = D / 16, DB = D / 32, kChunks = D / 8;      // k-steps, column blocks, 16-byte chunks of a bf16 row
@@ -111,7 +116,7 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
   // this lane's row
   const int iw = i0 + 32 * w, row = min(iw + l32, n_rows - 1);
   const int tq = quot(row, a.by_r), h = c * a.r + row - tq * a.r;
-  const int t = sr.s0 + tq, pos = min(p_first + tq, sr.keys - 1);
+  const int t = sr.s0 + tq, pos = min(p_first + tq, sr.keys - 1), n_seen = keys_up_to(a.window, p_first + tq, pos);
   const int w_lo = uni(p_first + quot(min(iw, n_rows - 1), a.by_r));               // positions of the wave's rows
   const int w_hi = uni(p_first + quot(min(iw + 32, n_rows) - 1, a.by_r));
   const bool idle = iw >= n_rows;
@@ -124,73 +129,106 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
     for (int k = 0; k < KS; ++k) qf[k] = src[2 * k + g32];
   }
 
-  const char* k_head = a.kc + c * a.kc_h * kEsz;
-  const char* v_head = a.vc + c * a.vc_h * kEsz;
+  const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz;
+  const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz;
+  const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
   const uint32_t smem_base = lds_addr(smem);
-  // Every wave looks up all 64 keys of a tile, one a lane; `seen` has a bit for each that exists.
-  auto look_up = [&](int n) __attribute__((always_inline)) {
-    return n < n1 ? cache_row(a, b, kt.tile(n) * kKeys + lane, kt.end) : CacheRow{-1, 0};
+  // Every wave looks up all 64 keys of a tile, one a lane, or the four groups of 16 of it; wave w stages the w-th 16 rows.
+  // bf16: global -> LDS, a lane's 16 bytes where the layout has the chunk; rows that are not there are zeros.  e4m3: through
+  // registers, 16 values to two chunks.
+  constexpr int kLine = E4M3 ? D / 16 : kChunks;                // 16-byte pieces of a cached row
+  constexpr int kRowsPer = 64 / kLine, kPass = 16 / kRowsPer;   // rows of a wave's load, and its loads
+  const int sub = lane / kLine;                                 // this lane's row of the first load
+  auto chunk_of = [&](int p) __attribute__((always_inline)) {   // its piece of the row (16 w rows further the layout is the same)
+    return E4M3 ? lane % kLine : D == 128 ? (lane & 15) ^ (sub << 2) ^ p : (lane & 7) ^ swz64((p * kRowsPer + sub) >> 1);
   };
-  auto seen_of = [&](const CacheRow& x) __attribute__((always_inline)) { return __builtin_amdgcn_ballot_w64(x.page >= 0); };
-
-  // ---- staging.  bf16: global -> LDS, a lane's 16 bytes where the layout has the chunk; rows that are not there are
-  // zeros.  e4m3: through registers, 16 values to two chunks.
-  constexpr int kRowsPer = 64 / kChunks;                        // rows one wave instruction fills (bf16): 4 or 8
-  constexpr int kPass = kKeys / (4 * kRowsPer);
-  constexpr int kLoads = kKeys * (D / 16) / 256;                // 16-value loads of a thread and tensor (e4m3): 2 or 1
-  uint4 k8[kLoads], v8[kLoads];
-  float ks8[kLoads], vs8[kLoads];
-  auto issue = [&](const CacheRow& x, int stage) __attribute__((always_inline)) {
-    const uint32_t dst = smem_base + stage * 2 * kTileBytes;
-    if constexpr (!E4M3) {
+  const uint32_t k_sub = (uint32_t)(sub * (int)a.kc_t * kEsz), v_sub = (uint32_t)(sub * (int)a.vc_t * kEsz);
+  struct Ahead {   // what is known of a tile before its loads go out: this lane's key, or the page of this wave's group
+    CacheRow row;
+    int page;
+  };
+  Plain plain{};
+  if constexpr (BY16) plain = plain_tiles<kKeys, 256>(a, b, kt, n0, n1, tid, flags);
+  auto look_up = [&](int n) __attribute__((always_inline)) {
+    Ahead x;
+    if constexpr (BY16) x.page = groups_of<1>(a, b, kt.tile(min(n, n1 - 1)) * kKeys + 16 * w).page[0];
+    else x.row = n < n1 ? cache_row(a, b, kt.tile(n) * kKeys + lane, kt.end) : CacheRow{-1, 0};
+    return x;
+  };
+  u32x4 k8[2][kPass], v8[2][kPass];                             // e4m3: two tiles on their way
+  float ks8[2][kPass], vs8[2][kPass];
+  // Starts the loads of tile n; a bit for each key that exists.
+  auto issue = [&](const Ahead& x, int n, int stage) __attribute__((always_inline)) {
+    const uint32_t dst = smem_base + stage * 2 * kTileBytes + w * kPass * 1024;
+    const uint64_t zero = zero_address();
+    if constexpr (BY16) {
+      const int j0 = kt.tile(min(n, n1 - 1)) * kKeys, at = place_of(a, j0 + 16 * w);
+      const uint64_t kb = k_head + group_off(x.page, at, a.kc_p * kEsz, a.kc_t * kEsz);
+      const uint64_t vb = v_head + group_off(x.page, at, a.vc_p * kEsz, a.vc_t * kEsz);
+      uint64_t seen = ~0ull;
+      const bool all = n >= plain.from && n < plain.to;
+      if (!all) seen = seen_of<4>(a, groups_of<4>(a, b, j0), j0, n < n1 ? kt.end : 0);
+      const uint32_t mine = (uint32_t)(seen >> (16 * w)) & 0xffffu;
 #pragma unroll
       for (int p = 0; p < kPass; ++p) {
-        const int slot = (p * 4 + w) * 64 + lane;               // 16-byte slot of the tile in LDS
-        int rr, chunk;
-        if constexpr (D == 128) {
-          rr = slot >> 4;
-          chunk = (slot & 15) ^ swz(rr);
+        const uint64_t kp = kb + p * kRowsPer * (uint32_t)(a.kc_t * kEsz);
+        const uint64_t vp = vb + p * kRowsPer * (uint32_t)(a.vc_t * kEsz);
+        const int rr = p * kRowsPer + sub, ch = chunk_of(p) * 16;
+        if constexpr (!E4M3) {
+          if (all) {
+            dma16s(uni64(kp), k_sub + ch, dst + p * 1024);
+            dma16s(uni64(vp), v_sub + ch, dst + p * 1024 + kTileBytes);
+          } else {
+            const bool there = mine >> rr & 1;
+            dma16(reinterpret_cast<const void*>((there ? kp + k_sub : zero) + ch), dst + p * 1024);
+            dma16(reinterpret_cast<const void*>((there ? vp + v_sub : zero) + ch), dst + p * 1024 + kTileBytes);
+          }
         } else {
-          const int R = slot >> 4;
-          rr = 2 * R + ((slot >> 3) & 1);
-          chunk = (slot & 7) ^ swz64(R);
+          const uint64_t ke = ke_head + x.page * a.ke_p + at * a.ke_t;
+          const uint64_t ve = ve_head + x.page * a.ve_p + at * a.ve_t;
+          const bool there = mine >> rr & 1;
+          k8[stage][p] = load16((there ? kp + k_sub : zero) + ch);
+          v8[stage][p] = load16((there ? vp + v_sub : zero) + ch);
+          ks8[stage][p] = load_scale(there ? ke + (uint32_t)(rr * (int)a.ke_t) : zero);
+          vs8[stage][p] = load_scale(there ? ve + (uint32_t)(rr * (int)a.ve_t) : zero);
         }
-        const int page = __shfl(x.page, rr), at = __shfl(x.at, rr);
-        const char* zero = reinterpret_cast<const char*>(zero_row);
-        const char* ks = page < 0 ? zero : k_head + (page * a.kc_p + at * a.kc_t) * 2;
-        const char* vs = page < 0 ? zero : v_head + (page * a.vc_p + at * a.vc_t) * 2;
-        dma16(ks + chunk * 16, dst + (p * 4 + w) * 1024);
-        dma16(vs + chunk * 16, dst + (p * 4 + w) * 1024 + kTileBytes);
       }
+      return seen;
     } else {
+      const CacheRow r = x.row;
 #pragma unroll
-      for (int p = 0; p < kLoads; ++p) {
-        const int i = p * 256 + tid, rr = i / (D / 16), chunk = i % (D / 16);
-        const int page = __shfl(x.page, rr), at = __shfl(x.at, rr);
-        k8[p] = v8[p] = uint4{0, 0, 0, 0};
-        ks8[p] = vs8[p] = 1.f;
-        if (page >= 0) {
-          k8[p] = *reinterpret_cast<const uint4*>(k_head + page * a.kc_p + at * a.kc_t + chunk * 16);
-          v8[p] = *reinterpret_cast<const uint4*>(v_head + page * a.vc_p + at * a.vc_t + chunk * 16);
-          ks8[p] = __uint_as_float((uint32_t)a.ke[page * a.ke_p + at * a.ke_t + c * a.ke_h] << 23);
-          vs8[p] = __uint_as_float((uint32_t)a.ve[page * a.ve_p + at * a.ve_t + c * a.ve_h] << 23);
+      for (int p = 0; p < kPass; ++p) {
+        const int rr = 16 * w + p * kRowsPer + sub, ch = chunk_of(p) * 16;
+        const int page = __shfl(r.page, rr), at = __shfl(r.at, rr);
+        const bool there = page >= 0;
+        const uint64_t ks = (there ? k_head + (page * a.kc_p + at * a.kc_t) * kEsz : zero) + ch;
+        const uint64_t vs = (there ? v_head + (page * a.vc_p + at * a.vc_t) * kEsz : zero) + ch;
+        if constexpr (!E4M3) {
+          dma16(reinterpret_cast<const void*>(ks), dst + p * 1024);
+          dma16(reinterpret_cast<const void*>(vs), dst + p * 1024 + kTileBytes);
+        } else {
+          k8[stage][p] = load16(ks);
+          v8[stage][p] = load16(vs);
+          ks8[stage][p] = load_scale(there ? ke_head + page * a.ke_p + at * a.ke_t : zero);
+          vs8[stage][p] = load_scale(there ? ve_head + page * a.ve_p + at * a.ve_t : zero);
         }
       }
+      return (uint64_t)__builtin_amdgcn_ballot_w64(r.page >= 0);
     }
   };
   auto land = [&](int stage) __attribute__((always_inline)) {   // e4m3: the loads of issue() into LDS
     if constexpr (E4M3) {
       char* dst = smem + stage * 2 * kTileBytes;
 #pragma unroll
-      for (int p = 0; p < kLoads; ++p) {
-        const int i = p * 256 + tid, rr = i / (D / 16), chunk = i % (D / 16);
+      for (int p = 0; p < kPass; ++p) {
+        const int rr = 16 * w + p * kRowsPer + sub;
         bf16x8 lo, hi;
-        widen(k8[p], ks8[p], lo, hi);
-        *reinterpret_cast<bf16x8*>(dst + L::off(rr, 2 * chunk)) = lo;
-        *reinterpret_cast<bf16x8*>(dst + L::off(rr, 2 * chunk + 1)) = hi;
-        widen(v8[p], vs8[p], lo, hi);
-        *reinterpret_cast<bf16x8*>(dst + kTileBytes + L::off(rr, 2 * chunk)) = lo;
-        *reinterpret_cast<bf16x8*>(dst + kTileBytes + L::off(rr, 2 * chunk + 1)) = hi;
+        widen(k8[stage][p], ks8[stage][p], lo, hi);
+        *reinterpret_cast<bf16x8*>(dst + L::off(rr, 2 * chunk_of(p))) = lo;
+        *reinterpret_cast<bf16x8*>(dst + L::off(rr, 2 * chunk_of(p) + 1)) = hi;
+        widen(v8[stage][p], vs8[stage][p], lo, hi);
+        *reinterpret_cast<bf16x8*>(dst + kTileBytes + L::off(rr, 2 * chunk_of(p))) = lo;
+        *reinterpret_cast<bf16x8*>(dst + kTileBytes + L::off(rr, 2 * chunk_of(p) + 1)) = hi;
       }
     }
   };
@@ -202,36 +240,35 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
   for (int db = 0; db < DB; ++db) o[db] = zero16();
   float m_run = first_max(c2), l_run = 0.f;
 
-  // e4m3: a tile is on its way to registers for a whole turn, and goes from there to LDS at the start of the next one
-  CacheRow next = look_up(n0);
-  uint64_t seen = 0, seen_1 = 0, seen_2 = 0;   // of tiles n, n + 1, n + 2
+  // e4m3: a tile is on its way to registers for two turns, and goes from there to LDS at the start of the turn before its own
+  Ahead next{};
+  uint64_t seen = 0, seen_1 = 0, seen_2 = 0, seen_3 = 0;   // of tiles n, n + 1, n + 2, n + 3
   if (n0 < n1) {
-    seen_1 = seen_of(next);
-    issue(next, 0);
-    land(0);
+    next = look_up(n0);
+    seen_1 = issue(next, n0, 0);
     next = look_up(n0 + 1);
     if constexpr (E4M3) {
-      seen_2 = seen_of(next);
-      issue(next, 1);
+      seen_2 = issue(next, n0 + 1, 1);
       next = look_up(n0 + 2);
+      land(0);
+      seen_3 = issue(next, n0 + 2, 0);
+      next = look_up(n0 + 3);
     }
   }
-  for (int n = n0; n < n1; ++n) {
-    const int stage = (n - n0) & 1;
+  auto turn = [&](auto stage_c, int n) __attribute__((always_inline)) {
+    constexpr int stage = decltype(stage_c)::value;
     if constexpr (!E4M3) wait_vmcnt0();   // this wave's part of tile n has landed
     __syncthreads();                      // everyone's part has landed; everyone left tile n - 1
     seen = seen_1;
     if constexpr (E4M3) {
       seen_1 = seen_2;
-      if (n + 1 < n1) land(stage ^ 1);
-      if (n + 2 < n1) {
-        seen_2 = seen_of(next);
-        issue(next, stage);
-        next = look_up(n + 3);
-      }
+      seen_2 = seen_3;
+      land(stage ^ 1);                    // tile n + 1 (past the end: zeros)
+      const Ahead x = next;
+      next = look_up(n + 4);              // ahead of the loads, so that waiting for it is not waiting for them
+      seen_3 = issue(x, n + 3, stage ^ 1);
     } else if (n + 1 < n1) {
-      seen_1 = seen_of(next);
-      issue(next, stage ^ 1);
+      seen_1 = issue(next, n + 1, stage ^ 1);
       next = look_up(n + 2);
     }
     const int j0 = kt.tile(n) * kKeys;
@@ -246,10 +283,8 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
         s0 = mfma32(lo.template rm<0>(Ks, k), qf[k], s0);
         s1 = mfma32(lo.template rm<32>(Ks, k), qf[k], s1);
       }
-      const bool windowed = a.window > 0 && j0 < w_hi - a.window + 1;
-      if (j0 + kKeys - 1 > w_lo || ~seen != 0 || windowed) {
-        mask_paged(s0, s1, j0 + 4 * g32, pos, windowed ? p_first + tq - a.window + 1 : 0, a.sinks, seen >> (4 * g32));
-      }
+      if (j0 + kKeys - 1 > w_lo || ~seen != 0 || (a.window > 0 && j0 < w_hi - a.window + 1))
+        mask_paged(s0, s1, j0 + 4 * g32, pos, n_seen, a.window > 0 ? a.sinks : 0, seen >> (4 * g32));
       // online softmax: the maximum is raised (and O rescaled) only when it grows by more than 2^8
       float ma = fmaxf(s0[0], s0[1]), mb = fmaxf(s1[0], s1[1]);
 #pragma unroll
@@ -291,6 +326,10 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
         o[db] = mfma32(lo.template tr<48>(Vs, db), pf[3], o[db]);
       }
     }
+  };
+  for (int n = n0; n < n1; n += 2) {
+    turn(std::integral_constant<int, 0>{}, n);
+    if (n + 1 < n1) turn(std::integral_constant<int, 1>{}, n + 1);
   }
   __syncthreads();
 
@@ -298,7 +337,7 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
   chunk_epilogue<D>(a, o, m_run * c2, l_run, smem + w * 32 * L::kRow, sr.s0, c, iw, n_rows, t, h, split, piece.count, lane);
 }
 
-// The same for 256 rows: eight waves and three stages, the walk of the eight-wave forward (D = 128).
+// The same for 256 rows: eight waves and three stages, the walk of the eight-wave forward (D = 128, pages of a multiple of 16).
 template <bool E4M3>
 __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_block) {
   constexpr int D = 128, kLog2 = 8, kRows8 = 1 << kLog2, kEsz = E4M3 ? 1 : 2, kStageBytes = 2 * kTileBytes;
@@ -322,7 +361,7 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
 
   const int iw = i0 + 32 * w, row = min(iw + l32, n_rows - 1);
   const int tq = quot(row, a.by_r), h = c * a.r + row - tq * a.r;
-  const int t = sr.s0 + tq, pos = min(p_first + tq, sr.keys - 1), p_row = p_first + tq;
+  const int t = sr.s0 + tq, pos = min(p_first + tq, sr.keys - 1), n_seen = keys_up_to(a.window, p_first + tq, pos);
   const int w_lo = uni(p_first + quot(min(iw, n_rows - 1), a.by_r));
   const int w_hi = uni(p_first + quot(min(iw + 32, n_rows) - 1, a.by_r));
   const bool idle = iw >= n_rows;
@@ -333,43 +372,58 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
 #pragma unroll
     for (int k = 0; k < 8; ++k) qf[k] = src[2 * k + g32];
   }
-  const char* k_head = a.kc + c * a.kc_h * kEsz;
-  const char* v_head = a.vc + c * a.vc_h * kEsz;
+  const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz;
+  const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz;
+  const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
   const uint32_t smem_base = lds_addr(smem);
+  // wave w stages rows 8 w .. 8 w + 7, half a group of 16
+  constexpr int kPass = E4M3 ? 1 : 2;
+  const int sub = E4M3 ? lane >> 3 : lane >> 4;
+  const uint32_t k_sub = (uint32_t)(sub * (int)a.kc_t * kEsz), v_sub = (uint32_t)(sub * (int)a.vc_t * kEsz);
+  __shared__ int flags[8];
+  const Plain plain = plain_tiles<kKeys, 512>(a, b, kt, n0, n0 + nt, tid, flags);
   auto look_up = [&](int n) __attribute__((always_inline)) {
-    return n < nt ? cache_row(a, b, kt.tile(n0 + n) * kKeys + lane, kt.end) : CacheRow{-1, 0};
+    return groups_of<1>(a, b, kt.tile(n0 + max(min(n, nt - 1), 0)) * kKeys + 8 * w).page[0];
   };
-  CacheRow next = look_up(0);
+  int next = look_up(0);
   uint64_t seen_a = 0, seen_b = 0;   // of the last two tiles issued
-  uint4 k8, v8;                      // e4m3: the tile on its way to LDS
+  u32x4 k8, v8;                      // e4m3: the tile on its way to LDS
   float ks8, vs8;
   auto issue = [&](int n, int stage) __attribute__((always_inline)) {
-    const CacheRow x = next;
-    seen_a = seen_b;
-    seen_b = __builtin_amdgcn_ballot_w64(x.page >= 0);
+    const int page = next;
     next = look_up(n + 1);
-    if constexpr (!E4M3) {
-      const uint32_t dst = smem_base + stage * kStageBytes;
+    const int j0 = kt.tile(n0 + n) * kKeys, at = place_of(a, j0 + 8 * w);
+    const bool all = n0 + n >= plain.from && n0 + n < plain.to;
+    seen_a = seen_b;
+    seen_b = ~0ull;
+    if (!all) seen_b = seen_of<4>(a, groups_of<4>(a, b, j0), j0, kt.end);
+    const uint32_t dst = smem_base + stage * kStageBytes + 8 * w * kRowBytes;
+    const uint64_t zero = zero_address();
+    const uint64_t kb = k_head + group_off(page, at, a.kc_p * kEsz, a.kc_t * kEsz);
+    const uint64_t vb = v_head + group_off(page, at, a.vc_p * kEsz, a.vc_t * kEsz);
+    const uint32_t mine = (uint32_t)(seen_b >> (8 * w)) & 0xffu;
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int rr = 32 * p + 4 * w + (lane >> 4), chunk = (lane & 15) ^ swz(rr);
-        const int page = __shfl(x.page, rr), at = __shfl(x.at, rr);
-        const char* zero = reinterpret_cast<const char*>(zero_row);
-        const char* ks = page < 0 ? zero : k_head + (page * a.kc_p + at * a.kc_t) * 2;
-        const char* vs = page < 0 ? zero : v_head + (page * a.vc_p + at * a.vc_t) * 2;
-        dma16(ks + chunk * 16, dst + (32 * p + 4 * w) * kRowBytes);
-        dma16(vs + chunk * 16, dst + (32 * p + 4 * w) * kRowBytes + kTileBytes);
+    for (int p = 0; p < kPass; ++p) {
+      const uint64_t kp = kb + 4 * p * (uint32_t)(a.kc_t * kEsz);
+      const uint64_t vp = vb + 4 * p * (uint32_t)(a.vc_t * kEsz);
+      const int ch = (E4M3 ? lane & 7 : (lane & 15) ^ swz(8 * (w & 1) + 4 * p + sub)) * 16;
+      const bool there = mine >> (4 * p + sub) & 1;
+      if constexpr (!E4M3) {
+        if (all) {
+          dma16s(uni64(kp), k_sub + ch, dst + 4 * p * kRowBytes);
+          dma16s(uni64(vp), v_sub + ch, dst + 4 * p * kRowBytes + kTileBytes);
+        } else {
+          dma16(reinterpret_cast<const void*>((there ? kp + k_sub : zero) + ch), dst + 4 * p * kRowBytes);
+          dma16(reinterpret_cast<const void*>((there ? vp + v_sub : zero) + ch), dst + 4 * p * kRowBytes + kTileBytes);
+        }
+      } else {
+        const uint64_t ke = ke_head + page * a.ke_p + at * a.ke_t;
+        const uint64_t ve = ve_head + page * a.ve_p + at * a.ve_t;
+        k8 = load16((there ? kp + k_sub : zero) + ch);
+        v8 = load16((there ? vp + v_sub : zero) + ch);
+        ks8 = load_scale(there ? ke + (uint32_t)(sub * (int)a.ke_t) : zero);
+        vs8 = load_scale(there ? ve + (uint32_t)(sub * (int)a.ve_t) : zero);
       }
-    } else {
-      const int rr = tid >> 3, chunk = tid & 7;
-      const int page = __shfl(x.page, rr), at = __shfl(x.at, rr);
-      const char* zero = reinterpret_cast<const char*>(zero_row);
-      const bool there = page >= 0;
-      k8 = *reinterpret_cast<const uint4*>((there ? k_head + page * a.kc_p + at * a.kc_t : zero) + chunk * 16);
-      v8 = *reinterpret_cast<const uint4*>((there ? v_head + page * a.vc_p + at * a.vc_t : zero) + chunk * 16);
-      const uint8_t* ze = reinterpret_cast<const uint8_t*>(zero);
-      ks8 = __uint_as_float((uint32_t)*(there ? a.ke + page * a.ke_p + at * a.ke_t + c * a.ke_h : ze) << 23);
-      vs8 = __uint_as_float((uint32_t)*(there ? a.ve + page * a.ve_p + at * a.ve_t + c * a.ve_h : ze) << 23);
     }
   };
   auto land = [&](int n) __attribute__((always_inline)) {
@@ -400,9 +454,8 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
           [&](f32x16& s0, f32x16& s1, int n) {
             const int j0 = kt.tile(n0 + n) * kKeys;
             const uint64_t seen = n + 1 < nt ? seen_a : seen_b;   // the tile after it is on its way already
-            const bool windowed = a.window > 0 && j0 < w_hi - a.window + 1;
-            if (j0 + kKeys - 1 > w_lo || ~seen != 0 || windowed)
-              mask_paged(s0, s1, j0 + 4 * g32, pos, windowed ? p_row - a.window + 1 : 0, a.sinks, seen >> (4 * g32));
+            if (j0 + kKeys - 1 > w_lo || ~seen != 0 || (a.window > 0 && j0 < w_hi - a.window + 1))
+              mask_paged(s0, s1, j0 + 4 * g32, pos, n_seen, a.window > 0 ? a.sinks : 0, seen >> (4 * g32));
           });
   __syncthreads();
   if (idle) return;
@@ -417,12 +470,12 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
 template <int D, bool E4M3>
 struct FewTile {
   static constexpr int N = D / (E4M3 ? 64 : 32);   // pieces of a key and lane
-  uint4 k[2][N], v[2][N];
+  u32x4 k[2][N], v[2][N];
   float ks[2], vs[2];                              // e4m3: scales
   uint32_t seen;                                   // a bit for each key that exists
 };
 
-template <int D, bool E4M3, int NQ>
+template <int D, bool E4M3, bool BY16, int NQ>
 __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* smem) {
   using T = FewTile<D, E4M3>;
   constexpr int TK = 32, kWaves = 4, kRow = D * 2, KF = D / 32, DB = D / 16;   // KF: operands of a key over D
@@ -436,8 +489,10 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
   const int n_rows = uni(sr.n * a.r), p_first = uni(sr.kv - sr.n);
   if (n_rows > a.few_rows) return;
 
-  const char* k_head = a.kc + c * a.kc_h * kEsz + 16 * q4;
-  const char* v_head = a.vc + c * a.vc_h * kEsz + 16 * q4;
+  const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz;
+  const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz;
+  const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
+  const uint32_t k_lane = (uint32_t)(c16 * (int)a.kc_t * kEsz + 16 * q4), v_lane = (uint32_t)(c16 * (int)a.vc_t * kEsz + 16 * q4);
   float* blocks = reinterpret_cast<float*>(smem);
   float* max_s = blocks + kWaves * 16 * NQ * kStride;                          // [wave][row]
   float* sum_s = max_s + kWaves * 16 * NQ;
@@ -458,28 +513,57 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
     const int per = piece.per, n0 = split * per, n1 = uni(min(kt.total, n0 + per));
     if (split > 0 && n0 >= n1) continue;
 
-    auto look_up = [&](int n, CacheRow (&x)[2]) __attribute__((always_inline)) {
+    struct Ahead {   // what is known of a tile before its loads go out
+      CacheRow row[2];
+      Groups<2> groups;
+    };
+    auto rows_of = [&](int n, CacheRow (&x)[2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) x[kb] = n < n1 ? cache_row(a, b, kt.tile(n) * TK + 16 * kb + c16, kt.end) : CacheRow{-1, 0};
     };
-    auto load = [&](T& t, const CacheRow (&x)[2]) __attribute__((always_inline)) {
-      t.seen = ((uint32_t)__builtin_amdgcn_ballot_w64(x[0].page >= 0) & 0xffffu) |
-               ((uint32_t)__builtin_amdgcn_ballot_w64(x[1].page >= 0) << 16);
+    auto look_up = [&](int n, Ahead& x) __attribute__((always_inline)) {
+      if constexpr (BY16) x.groups = groups_of<2>(a, b, kt.tile(max(min(n, n1 - 1), 0)) * TK);
+      else rows_of(n, x.row);
+    };
+    auto load = [&](T& t, const Ahead& x, int n) __attribute__((always_inline)) {
+      const uint64_t zero = zero_address();
+      int j0 = 0;
+      if constexpr (BY16) {
+        j0 = kt.tile(max(min(n, n1 - 1), 0)) * TK;
+        t.seen = (uint32_t)seen_of<2>(a, x.groups, j0, n < n1 ? kt.end : 0);
+      } else {
+        t.seen = ((uint32_t)__builtin_amdgcn_ballot_w64(x.row[0].page >= 0) & 0xffffu) |
+                 ((uint32_t)__builtin_amdgcn_ballot_w64(x.row[1].page >= 0) << 16);
+      }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const bool there = x[kb].page >= 0;
-        const char* zero = reinterpret_cast<const char*>(zero_row);
-        const char* kp = there ? k_head + (x[kb].page * a.kc_p + x[kb].at * a.kc_t) * kEsz : zero;
-        const char* vp = there ? v_head + (x[kb].page * a.vc_p + x[kb].at * a.vc_t) * kEsz : zero;
+        uint64_t kp, vp, ke = zero, ve = zero;
+        if constexpr (BY16) {
+          const int page = x.groups.page[kb], at = place_of(a, j0 + 16 * kb);
+          const bool there = t.seen >> (16 * kb + c16) & 1;
+          kp = there ? k_head + (page * a.kc_p + at * a.kc_t) * kEsz + k_lane : zero + 16 * q4;
+          vp = there ? v_head + (page * a.vc_p + at * a.vc_t) * kEsz + v_lane : zero + 16 * q4;
+          if constexpr (E4M3) {
+            ke = there ? ke_head + page * a.ke_p + at * a.ke_t + (uint32_t)(c16 * (int)a.ke_t) : zero;
+            ve = there ? ve_head + page * a.ve_p + at * a.ve_t + (uint32_t)(c16 * (int)a.ve_t) : zero;
+          }
+        } else {
+          const CacheRow r = x.row[kb];
+          const bool there = r.page >= 0;
+          kp = (there ? k_head + (r.page * a.kc_p + r.at * a.kc_t) * kEsz : zero) + 16 * q4;
+          vp = (there ? v_head + (r.page * a.vc_p + r.at * a.vc_t) * kEsz : zero) + 16 * q4;
+          if constexpr (E4M3) {
+            ke = there ? ke_head + r.page * a.ke_p + r.at * a.ke_t : zero;
+            ve = there ? ve_head + r.page * a.ve_p + r.at * a.ve_t : zero;
+          }
+        }
 #pragma unroll
-        for (int i = 0; i < T::N; ++i) t.k[kb][i] = *reinterpret_cast<const uint4*>(kp + 64 * i);
+        for (int i = 0; i < T::N; ++i) t.k[kb][i] = load16(kp + 64 * i);
 #pragma unroll
-        for (int i = 0; i < T::N; ++i) t.v[kb][i] = *reinterpret_cast<const uint4*>(vp + 64 * i);
+        for (int i = 0; i < T::N; ++i) t.v[kb][i] = load16(vp + 64 * i);
         if constexpr (E4M3) {
-          const uint8_t* ke = there ? a.ke + x[kb].page * a.ke_p + x[kb].at * a.ke_t + c * a.ke_h : reinterpret_cast<const uint8_t*>(zero);
-          const uint8_t* ve = there ? a.ve + x[kb].page * a.ve_p + x[kb].at * a.ve_t + c * a.ve_h : reinterpret_cast<const uint8_t*>(zero);
-          t.ks[kb] = __uint_as_float((uint32_t)*ke << 23);
-          t.vs[kb] = __uint_as_float((uint32_t)*ve << 23);
+          t.ks[kb] = load_scale(ke);
+          t.vs[kb] = load_scale(ve);
         }
       }
     };
@@ -487,18 +571,18 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
     // this wave's tiles: n0 + w, n0 + w + 4, ..
     // The look-up of a tile goes out ahead of the loads of the tile before it, so that waiting for it is not waiting for them.
     T ta, tb;
-    CacheRow at[2], at_next[2];
+    Ahead at{}, at_next{};
     look_up(n0 + w, at);
     look_up(n0 + w + kWaves, at_next);
-    load(ta, at);
+    load(ta, at, n0 + w);
 
     bf16x8 qf[NQ][KF];
-    int pos[NQ], p_row[NQ];
+    int pos[NQ], n_seen[NQ];
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) {
       const int row = min(i0 + 16 * qb + c16, n_rows - 1), tq = quot(row, a.by_r), h = c * a.r + row - tq * a.r;
-      p_row[qb] = p_first + tq;
-      pos[qb] = min(p_row[qb], sr.keys - 1);
+      pos[qb] = min(p_first + tq, sr.keys - 1);
+      n_seen[qb] = keys_up_to(a.window, p_first + tq, pos[qb]);
       const __bf16* q = static_cast<const __bf16*>(a.q) + (sr.s0 + tq) * a.q_t + h * a.q_h;
 #pragma unroll
       for (int f = 0; f < KF; ++f)
@@ -515,10 +599,9 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
     const float c2 = a.scale_log2;
 
     auto step = [&](T& cur, T& nxt, int n) __attribute__((always_inline)) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) at[kb] = at_next[kb];
+      at = at_next;
       look_up(n + 2 * kWaves, at_next);
-      if constexpr (NQ == 1) load(nxt, at);   // (past the end: zeros)
+      if constexpr (NQ == 1) load(nxt, at, n + kWaves);   // (past the end: zeros)
       const int j0 = kt.tile(n) * TK;
       const uint32_t seen = cur.seen;
       // V into LDS, K as operands
@@ -538,7 +621,7 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
         } else {
 #pragma unroll
           for (int i = 0; i < T::N; ++i) {
-            *reinterpret_cast<uint4*>(Vs + Tile<D>::off(16 * kb + c16, q4 + 4 * i)) = cur.v[kb][i];
+            *reinterpret_cast<u32x4*>(Vs + Tile<D>::off(16 * kb + c16, q4 + 4 * i)) = cur.v[kb][i];
             kf[i] = __builtin_bit_cast(bf16x8, cur.k[kb][i]);
           }
         }
@@ -550,25 +633,35 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
         }
       }
       wave_lds_order();
-      if constexpr (NQ > 1) load(nxt, at);
-      const bool windowed = a.window > 0 && j0 < p_hi - a.window + 1;
-      const bool masked = j0 + TK - 1 > p_lo || ~seen != 0 || windowed;
+      if constexpr (NQ > 1) load(nxt, at, n + kWaves);
+      const bool masked = j0 + TK - 1 > p_lo || ~seen != 0 || (a.window > 0 && j0 < p_hi - a.window + 1);
       const uint32_t seen_l = seen >> (4 * q4);
+      const int sinks = a.window > 0 ? a.sinks : 0;
       bf16x8 pf[NQ];
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb) {
-        const int first = windowed ? p_row[qb] - a.window + 1 : 0;
         float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = sc[kb][qb][e] * c2;
-            const int key = j0 + 16 * kb + 4 * q4 + e;
-            if (masked && !(key <= pos[qb] && (key >= first || key < a.sinks) && (seen_l >> (16 * kb + e) & 1))) x = -INFINITY;
-            sc[kb][qb][e] = x;
-            mx = fmaxf(mx, x);
-          }
+          for (int e = 0; e < 4; ++e) sc[kb][qb][e] *= c2;
+        if (masked) {
+          int d0 = pos[qb] - j0 - 4 * q4;
+          asm volatile("" : "+v"(d0));
+          const int last = min(pos[qb], sinks - 1) - j0 - 4 * q4;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int bit = 16 * kb + e;
+              const bool in = (((unsigned)(d0 - bit) < (unsigned)n_seen[qb]) | (bit <= last)) & (seen_l >> bit & 1);
+              sc[kb][qb][e] = in ? sc[kb][qb][e] : -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[kb][qb][e]);
         mx = max_of_4(mx);
         if (__builtin_amdgcn_ballot_w64(mx > m_run[qb]) != 0) {
           const float m_new = fmaxf(m_run[qb], mx);
@@ -661,47 +754,53 @@ constexpr int kChunkBytes = 4 * kKeys * Tile<D>::kRow;
 template <int D, int NQ>
 constexpr int kFewBytes = 4 * 16 * NQ * (D + 4 + 2) * 4 > 4 * 32 * D * 2 ? 4 * 16 * NQ * (D + 4 + 2) * 4 : 4 * 32 * D * 2;
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool BY16>
 __global__ void __launch_bounds__(256, 2) paged_chunk_kernel(PArgs a, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D>];
-  chunk_workgroup<D, E4M3>(a, first_block + block_id(), smem);
+  __shared__ int flags[4];
+  chunk_workgroup<D, E4M3, BY16>(a, first_block + block_id(), smem, flags);
 }
 
-template <int D, bool E4M3, int NQ>
+template <int D, bool E4M3, bool BY16, int NQ>
 __global__ void __launch_bounds__(256, 2) paged_few_kernel(PArgs a, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[kFewBytes<D, NQ>];
-  few_workgroup<D, E4M3, NQ>(a, first_block + block_id(), smem);
+  few_workgroup<D, E4M3, BY16, NQ>(a, first_block + block_id(), smem);
 }
 
-template <int D, bool E4M3>
-__global__ void __launch_bounds__(256, 2) paged_both_kernel(PArgs a, int first_block) {
+template <int D, bool E4M3, bool BY16>
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_both_kernel(PArgs a, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D> > kFewBytes<D, 2> ? kChunkBytes<D> : kFewBytes<D, 2>];
+  __shared__ int flags[4];
   const int block = first_block + block_id();
-  if (block < a.chunk_blocks)
-    chunk_workgroup<D, E4M3>(a, block, smem);
+  if (block < a.chunk_blocks)   // the long chains first: 62 us, the others first 72 (16 sequences of 1 to 600 rows, window 4096)
+    chunk_workgroup<D, E4M3, BY16>(a, block, smem, flags);
   else
-    few_workgroup<D, E4M3, 2>(a, block - a.chunk_blocks, smem);
+    few_workgroup<D, E4M3, BY16, 2>(a, block - a.chunk_blocks, smem);
 }
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool BY16>
 int launch_t(const PArgs& a, int nq, hipStream_t st) {
   const int few = a.B * a.Hkv * a.few.splits;
-  if constexpr (D == 128) {
+  if constexpr (D == 128 && BY16) {
     if (a.chunk_blocks > 0 && a.chunk_rows == 256) {
       const int rc = launch_blocks(paged_long_kernel<E4M3>, a.chunk_blocks, 512, st, a);
-      return rc != 0 || a.few_rows == 0 ? rc : launch_blocks(paged_few_kernel<D, E4M3, 2>, few, 256, st, a);
+      return rc != 0 || a.few_rows == 0 ? rc : launch_blocks(paged_few_kernel<D, E4M3, BY16, 2>, few, 256, st, a);
     }
   }
-  if (a.few_rows == 0) return launch_blocks(paged_chunk_kernel<D, E4M3>, a.chunk_blocks, 256, st, a);
-  if (a.chunk_blocks > 0) return launch_blocks(paged_both_kernel<D, E4M3>, a.chunk_blocks + few, 256, st, a);
-  return nq == 1 ? launch_blocks(paged_few_kernel<D, E4M3, 1>, few, 256, st, a) : launch_blocks(paged_few_kernel<D, E4M3, 2>, few, 256, st, a);
+  if (a.few_rows == 0) return launch_blocks(paged_chunk_kernel<D, E4M3, BY16>, a.chunk_blocks, 256, st, a);
+  if (a.chunk_blocks > 0) return launch_blocks(paged_both_kernel<D, E4M3, BY16>, a.chunk_blocks + few, 256, st, a);
+  return nq == 1 ? launch_blocks(paged_few_kernel<D, E4M3, BY16, 1>, few, 256, st, a) : launch_blocks(paged_few_kernel<D, E4M3, BY16, 2>, few, 256, st, a);
+}
+template <int D, bool E4M3>
+int launch_pages(const PArgs& a, int nq, hipStream_t st) {
+  return a.by16 ? launch_t<D, E4M3, true>(a, nq, st) : launch_t<D, E4M3, false>(a, nq, st);
 }
 
 }  // namespace
 
 int launch_paged_bf16(const PArgs& a, int D, bool e4m3, int nq, hipStream_t st) {
-  if (D == 64) return e4m3 ? launch_t<64, true>(a, nq, st) : launch_t<64, false>(a, nq, st);
-  return e4m3 ? launch_t<128, true>(a, nq, st) : launch_t<128, false>(a, nq, st);
+  if (D == 64) return e4m3 ? launch_pages<64, true>(a, nq, st) : launch_pages<64, false>(a, nq, st);
+  return e4m3 ? launch_pages<128, true>(a, nq, st) : launch_pages<128, false>(a, nq, st);
 }
 
 }  // namespace s2

@@ -39,14 +39,15 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
 
   const int iw = i0 + 16 * w, row = min(iw + c16, n_rows - 1);
   const int tq = quot(row, a.by_r), h = c * a.r + row - tq * a.r;
-  const int t = sr.s0 + tq, pos = min(p_first + tq, sr.keys - 1);
+  const int t = sr.s0 + tq, pos = min(p_first + tq, sr.keys - 1), n_seen = keys_up_to(a.window, p_first + tq, pos);
   const int w_lo = uni(p_first + quot(min(iw, n_rows - 1), a.by_r));
   const int w_hi = uni(p_first + quot(min(iw + 16, n_rows) - 1, a.by_r));
   const bool idle = iw >= n_rows;
   const float c2 = a.scale_log2;
 
-  const char* k_head = a.kc + c * a.kc_h * kEsz;
-  const char* v_head = a.vc + c * a.vc_h * kEsz;
+  const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz;
+  const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz;
+  const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
   const uint32_t base = lds_addr(smem);
   // every wave looks up the 32 keys of a tile, twice; `seen` has a bit for each that exists
   auto look_up = [&](int n) __attribute__((always_inline)) {
@@ -58,7 +59,7 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   ln.init(lane, w);
   constexpr int kLoads = kTile * (D / 16) / 256 > 0 ? kTile * (D / 16) / 256 : 1;   // e4m3: 16-value loads of a thread
   constexpr bool kAll = kTile * (D / 16) >= 256;                                    // else the upper half of the threads has none
-  uint4 k8[kLoads], v8[kLoads];
+  u32x4 k8[kLoads], v8[kLoads];
   float ks8[kLoads], vs8[kLoads];
   auto issue = [&](const CacheRow& x, int stage) __attribute__((always_inline)) {
     const uint32_t dst = base + stage * 2 * L::kTileBytes;
@@ -68,25 +69,23 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
       for (int p = 0; p < kTile / kStep; ++p) {
         const int rr = p * kStep + ln.st_row;
         const int page = __shfl(x.page, rr), at = __shfl(x.at, rr);
-        const char* zero = reinterpret_cast<const char*>(zero_row);
-        const char* ks = page < 0 ? zero : k_head + (page * a.kc_p + at * a.kc_t) * 4;
-        const char* vs = page < 0 ? zero : v_head + (page * a.vc_p + at * a.vc_t) * 4;
-        dma16(ks + (ln.st_chunk << 4), dst + (p * 4 + w) * 1024);
-        dma16(vs + (ln.st_chunk << 4), dst + (p * 4 + w) * 1024 + L::kTileBytes);
+        const uint64_t zero = zero_address();
+        const uint64_t ks = page < 0 ? zero : k_head + (page * a.kc_p + at * a.kc_t) * 4;
+        const uint64_t vs = page < 0 ? zero : v_head + (page * a.vc_p + at * a.vc_t) * 4;
+        dma16(reinterpret_cast<const void*>(ks + (ln.st_chunk << 4)), dst + (p * 4 + w) * 1024);
+        dma16(reinterpret_cast<const void*>(vs + (ln.st_chunk << 4)), dst + (p * 4 + w) * 1024 + L::kTileBytes);
       }
     } else {
 #pragma unroll
       for (int p = 0; p < kLoads; ++p) {
         const int i = p * 256 + tid, rr = i / (D / 16), chunk = i % (D / 16);
         const int page = __shfl(x.page, rr & 31), at = __shfl(x.at, rr & 31);
-        k8[p] = v8[p] = uint4{0, 0, 0, 0};
-        ks8[p] = vs8[p] = 1.f;
-        if (page >= 0 && (kAll || rr < kTile)) {
-          k8[p] = *reinterpret_cast<const uint4*>(k_head + page * a.kc_p + at * a.kc_t + chunk * 16);
-          v8[p] = *reinterpret_cast<const uint4*>(v_head + page * a.vc_p + at * a.vc_t + chunk * 16);
-          ks8[p] = __uint_as_float((uint32_t)a.ke[page * a.ke_p + at * a.ke_t + c * a.ke_h] << 23);
-          vs8[p] = __uint_as_float((uint32_t)a.ve[page * a.ve_p + at * a.ve_t + c * a.ve_h] << 23);
-        }
+        const uint64_t zero = zero_address();
+        const bool there = page >= 0 && (kAll || rr < kTile);
+        k8[p] = load16((there ? k_head + page * a.kc_p + at * a.kc_t : zero) + chunk * 16);
+        v8[p] = load16((there ? v_head + page * a.vc_p + at * a.vc_t : zero) + chunk * 16);
+        ks8[p] = load_scale(there ? ke_head + page * a.ke_p + at * a.ke_t : zero);
+        vs8[p] = load_scale(there ? ve_head + page * a.ve_p + at * a.ve_t : zero);
       }
     }
   };
@@ -99,7 +98,7 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
         if (kAll || rr < kTile) {
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
-            const uint4 u = kv ? v8[p] : k8[p];
+            const u32x4 u = kv ? v8[p] : k8[p];
             const float s = kv ? vs8[p] : ks8[p];
             const uint32_t x[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -148,21 +147,28 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
       const char* Vs = Ks + L::kTileBytes;
       f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
       scores<D>(sc, Ks, ln, qf);
-      const bool windowed = a.window > 0 && j0 < w_hi - a.window + 1;
-      const bool masked = j0 + kTile - 1 > w_lo || ~seen != 0 || windowed;
-      const int first = windowed ? p_first + tq - a.window + 1 : 0;
-      const uint32_t seen_l = seen >> (4 * q4);
+      const bool masked = j0 + kTile - 1 > w_lo || ~seen != 0 || (a.window > 0 && j0 < w_hi - a.window + 1);
       float mx = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) sc[kb] *= c2;
+      if (masked) {
+        int d0 = pos - j0 - 4 * q4;
+        asm volatile("" : "+v"(d0));   // keeps the compiler from doing this ahead of the branch
+        const int last = min(pos, (a.window > 0 ? a.sinks : 0) - 1) - j0 - 4 * q4;
+        const uint32_t seen_l = seen >> (4 * q4);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int bit = 16 * kb + v;
+            const bool in = (((unsigned)(d0 - bit) < (unsigned)n_seen) | (bit <= last)) & (seen_l >> bit & 1);
+            sc[kb][v] = in ? sc[kb][v] : -INFINITY;
+          }
+      }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          float x = sc[kb][v] * c2;
-          const int key = j0 + 16 * kb + 4 * q4 + v;
-          if (masked && !(key <= pos && (key >= first || key < a.sinks) && (seen_l >> (16 * kb + v) & 1))) x = -INFINITY;
-          sc[kb][v] = x;
-          mx = fmaxf(mx, x);
-        }
+        for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[kb][v]);
       mx = max_cols(mx);
       if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
         const float m_new = fmaxf(m_run, mx);
@@ -207,7 +213,7 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
 //   V  lane (c16, q4) has keys 4 q4 + v, values 64 j + 4 c16 ..
 template <int D, bool E4M3>
 struct FewTile {
-  uint4 k[E4M3 ? D / 64 : D / 16];
+  u32x4 k[E4M3 ? D / 64 : D / 16];
   uint32_t v8[4][D / 64];
   f32x4 v[4][D / 64];
   float ks, vs[4];
@@ -228,8 +234,9 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
   if (b >= a.B) return;
   const SeqRows sr = seq_rows(a, b);
   const int n_rows = uni(sr.n * a.r), p_first = uni(sr.kv - sr.n);
-  const char* k_head = a.kc + c * a.kc_h * kEsz + 16 * q4;
-  const char* v_head = a.vc + c * a.vc_h * kEsz + 4 * c16 * kEsz;
+  const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz + 16 * q4;
+  const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz + 4 * c16 * kEsz;
+  const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
   const float c2 = a.scale_log2;
 
   for (int i0 = 0; i0 < n_rows; i0 += 16) {
@@ -244,22 +251,21 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
     };
     auto load = [&](T& t, const CacheRow& x) __attribute__((always_inline)) {
       t.seen = (uint32_t)__builtin_amdgcn_ballot_w64(x.page >= 0) & 0xffffu;
-      const char* zero = reinterpret_cast<const char*>(zero_row);
-      const uint8_t* ze = reinterpret_cast<const uint8_t*>(zero);
-      const char* kp = x.page >= 0 ? k_head + (x.page * a.kc_p + x.at * a.kc_t) * kEsz : zero;
+      const uint64_t zero = zero_address();
+      const uint64_t kp = x.page >= 0 ? k_head + (x.page * a.kc_p + x.at * a.kc_t) * kEsz : zero;
 #pragma unroll
-      for (int i = 0; i < (E4M3 ? D / 64 : D / 16); ++i) t.k[i] = *reinterpret_cast<const uint4*>(kp + 64 * i);
-      if constexpr (E4M3) t.ks = __uint_as_float((uint32_t)*(x.page >= 0 ? a.ke + x.page * a.ke_p + x.at * a.ke_t + c * a.ke_h : ze) << 23);
+      for (int i = 0; i < (E4M3 ? D / 64 : D / 16); ++i) t.k[i] = load16(kp + 64 * i);
+      if constexpr (E4M3) t.ks = load_scale(x.page >= 0 ? ke_head + x.page * a.ke_p + x.at * a.ke_t : zero);
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const int page = __shfl(x.page, 4 * q4 + v), at = __shfl(x.at, 4 * q4 + v);
-        const char* vp = page >= 0 ? v_head + (page * a.vc_p + at * a.vc_t) * kEsz : zero;
+        const uint64_t vp = page >= 0 ? v_head + (page * a.vc_p + at * a.vc_t) * kEsz : zero;
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
-          if constexpr (E4M3) t.v8[v][j] = *reinterpret_cast<const uint32_t*>(vp + 64 * j);
-          else t.v[v][j] = *reinterpret_cast<const f32x4*>(vp + 256 * j);
+          if constexpr (E4M3) t.v8[v][j] = S2_GLOBAL(uint32_t, vp + 64 * j);
+          else t.v[v][j] = S2_GLOBAL(f32x4, vp + 256 * j);
         }
-        if constexpr (E4M3) t.vs[v] = __uint_as_float((uint32_t)*(page >= 0 ? a.ve + page * a.ve_p + at * a.ve_t + c * a.ve_h : ze) << 23);
+        if constexpr (E4M3) t.vs[v] = load_scale(page >= 0 ? ve_head + page * a.ve_p + at * a.ve_t : zero);
       }
     };
     auto widen4 = [](uint32_t u, float s) __attribute__((always_inline)) {
@@ -272,7 +278,7 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
     CacheRow at = look_up(n0 + w), at_next = look_up(n0 + w + kWaves);
     load(ta, at);
     const int row = min(i0 + c16, n_rows - 1), tq = quot(row, a.by_r), h = c * a.r + row - tq * a.r;
-    const int p_row = p_first + tq, pos = min(p_row, sr.keys - 1), t = sr.s0 + tq;
+    const int pos = min(p_first + tq, sr.keys - 1), n_seen = keys_up_to(a.window, p_first + tq, pos), t = sr.s0 + tq;
     f32x4 qf[D / 16];
     {
       const float* q = static_cast<const float*>(a.q) + t * a.q_t + h * a.q_h;
@@ -297,7 +303,7 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
       for (int i = 0; i < D / 16; ++i) {
         f32x4 x;
         if constexpr (E4M3) {
-          const uint4 u = cur.k[i >> 2];
+          const u32x4 u = cur.k[i >> 2];
           x = widen4((i & 3) == 0 ? u.x : (i & 3) == 1 ? u.y : (i & 3) == 2 ? u.z : u.w, cur.ks);
         } else {
           x = __builtin_bit_cast(f32x4, cur.k[i]);
@@ -309,19 +315,22 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
         }
       }
       sc += odd;
-      const bool windowed = a.window > 0 && j0 < p_hi - a.window + 1;
-      const bool masked = j0 + TK - 1 > p_lo || cur.seen != 0xffffu || windowed;
-      const int first = windowed ? p_row - a.window + 1 : 0;
-      const uint32_t seen_l = cur.seen >> (4 * q4);
+      const bool masked = j0 + TK - 1 > p_lo || cur.seen != 0xffffu || (a.window > 0 && j0 < p_hi - a.window + 1);
       float mx = -INFINITY;
+      sc *= c2;
+      if (masked) {
+        int d0 = pos - j0 - 4 * q4;
+        asm volatile("" : "+v"(d0));
+        const int last = min(pos, (a.window > 0 ? a.sinks : 0) - 1) - j0 - 4 * q4;
+        const uint32_t seen_l = cur.seen >> (4 * q4);
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        float x = sc[v] * c2;
-        const int key = j0 + 4 * q4 + v;
-        if (masked && !(key <= pos && (key >= first || key < a.sinks) && (seen_l >> v & 1))) x = -INFINITY;
-        sc[v] = x;
-        mx = fmaxf(mx, x);
+        for (int v = 0; v < 4; ++v) {
+          const bool in = (((unsigned)(d0 - v) < (unsigned)n_seen) | (v <= last)) & (seen_l >> v & 1);
+          sc[v] = in ? sc[v] : -INFINITY;
+        }
       }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) mx = fmaxf(mx, sc[v]);
       mx = max_cols(mx);
       if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
         const float m_new = fmaxf(m_run, mx);
@@ -399,12 +408,12 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
   }
 }
 
-// o = sum of the pieces' outputs by their share exp2(lse_s - lse) of the row.  D / 4 lanes hold a piece's output; of a workgroup's
-// groups of so many lanes G take the pieces of one row (each with a running maximum of its own), the others other heads of the
-// same token, `heads` of them to a workgroup.
-template <int D, int TK, int FEW_TK, bool BF16, int G>
+// o = sum of the pieces' outputs by their share exp2(lse_s - lse) of the row.  D / 4 lanes hold a piece's output; G groups of so
+// many lanes take the pieces of one row, four at a time (each group with a running maximum of its own), the other groups of a
+// workgroup other heads of the same token, `heads` of them to a workgroup.
+template <int D, int TK, int FEW_TK, bool BF16>
 __global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, int nq, int heads, int head_blocks, Div by_head_blocks, int first_block) {
-  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAtOnce = kGroups / G;
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
   __shared__ float4 acc_s[kGroups][kLanes];
   __shared__ float m_s[kGroups], l_s[kGroups];
   const int tid = thread_id(), H = a.Hkv * a.r;
@@ -419,9 +428,10 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, int nq, int he
   const int tile = few ? 16 * nq : a.chunk_rows;
   const PSet& set = few ? a.few : a.chunk;
   if (set.splits == 1) return;                    // in one piece: written by the attention kernel
-  const int g = tid / kLanes, l = tid % kLanes, sub = g / G, piece0 = g % G;
+  const int log2g = set.splits <= 4 ? 0 : set.splits <= 8 ? 1 : set.splits <= 16 ? 2 : 3;
+  const int g = tid / kLanes, l = tid % kLanes, sub = g >> log2g, piece0 = g & ((1 << log2g) - 1);
   const size_t step = (size_t)a.T * H;
-  for (int hh = 0; hh < heads; hh += kAtOnce) {
+  for (int hh = 0; hh < heads; hh += kGroups >> log2g) {
     const int h = h0 + hh + sub;
     const bool on = hh + sub < heads && h < H;
     const int i = (t - sr.s0) * a.r + (h - quot(h, a.by_r) * a.r), j0 = i & ~(tile - 1);   // tile: a power of two
@@ -433,12 +443,12 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, int nq, int he
     const float* pl = a.part_lse + (size_t)t * H + h;
     float m = -FLT_MAX, sum = 0.f;
     float4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = piece0; s0 < pieces; s0 += 4 * G) {
+    for (int s0 = piece0; s0 < pieces; s0 += 4 << log2g) {
       float ls[4];
       float4 x[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int s = s0 + u * G;
+        const int s = s0 + (u << log2g);
         ls[u] = s < pieces ? pl[s * step] : -INFINITY;
         x[u] = s < pieces ? *reinterpret_cast<const float4*>(po + s * step * D) : float4{0.f, 0.f, 0.f, 0.f};
       }
@@ -455,18 +465,16 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, int nq, int he
         acc.z = fmaf(x[u].z, f, acc.z); acc.w = fmaf(x[u].w, f, acc.w);
       }
     }
-    if constexpr (G > 1) {
+    if (log2g > 0) {
       acc_s[g][l] = acc;
       if (l == 0) { m_s[g] = m; l_s[g] = sum; }
       __syncthreads();
       if (piece0 == 0) {
         float top = m;
-#pragma unroll
-        for (int x = 1; x < G; ++x) top = fmaxf(top, m_s[g + x]);
+        for (int x = 1; x < 1 << log2g; ++x) top = fmaxf(top, m_s[g + x]);
         sum = 0.f;
         acc = float4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < G; ++x) {
+        for (int x = 0; x < 1 << log2g; ++x) {
           const float f = exp2f(m_s[g + x] - top);
           sum = fmaf(l_s[g + x], f, sum);
           acc.x = fmaf(acc_s[g + x][l].x, f, acc.x); acc.y = fmaf(acc_s[g + x][l].y, f, acc.y);
@@ -491,17 +499,11 @@ template <int D, int TK, int FEW_TK, bool BF16>
 int join_t(const PArgs& a, int nq, hipStream_t st) {
   constexpr int kGroups = 1024 / D;
   const int H = a.Hkv * a.r, splits = a.few.splits > a.chunk.splits ? a.few.splits : a.chunk.splits;
-  // four pieces in flight to a group; heads go together while 1024 workgroups are left
-  const int G = splits <= 4 ? 1 : splits <= 8 ? 2 : splits <= 16 ? 4 : 8;
-  int heads = kGroups / G;
+  // heads go together while 1024 workgroups are left
+  int heads = splits <= 4 ? kGroups : splits <= 8 ? kGroups / 2 : splits <= 16 ? kGroups / 4 : kGroups / 8;
   while (2 * heads <= H && (long long)a.T * (H / (2 * heads)) >= 1024) heads *= 2;
   const int head_blocks = (H + heads - 1) / heads;
-  const Div d = div_by(head_blocks);
-  const int blocks = a.T * head_blocks;
-  if (G == 1) return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 1>, blocks, 256, st, a, nq, heads, head_blocks, d);
-  if (G == 2) return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 2>, blocks, 256, st, a, nq, heads, head_blocks, d);
-  if (G == 4) return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 4>, blocks, 256, st, a, nq, heads, head_blocks, d);
-  return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16, 8>, blocks, 256, st, a, nq, heads, head_blocks, d);
+  return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16>, a.T * head_blocks, 256, st, a, nq, heads, head_blocks, div_by(head_blocks));
 }
 
 }  // namespace
