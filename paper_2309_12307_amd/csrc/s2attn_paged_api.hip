@@ -77,7 +77,7 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   Plan x{};
   const long long r = p->H / p->Hkv, rows = p->T * r, seqs = std::max(1, std::min(p->B, p->T));
   // One token a sequence (as far as T and B tell): all go to `few`, which takes any number of rows, by turns.  Where some have
-  // more, those of up to 32 rows go there and the others to `chunk`.
+  // more, those of up to 16 or 32 rows go there and the others to `chunk`.
   // (fp32: all to one of the two.)
   const bool f32 = p->dtype == S2ATTN_F32;
   x.nq = 1;
@@ -88,8 +88,8 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   } else {
     x.chunk = true;
     x.few = !f32 && p->B > 1;
-    x.nq = 2;
-    x.few_rows = x.few ? 32 : 0;
+    x.nq = rows <= 16 * seqs ? 1 : 2;
+    x.few_rows = x.few ? 16 * x.nq : 0;
   }
   const long long most = (long long)p->table_cols * p->page_size;
   long long keys = p->max_kv > 0 ? std::min<long long>(p->max_kv, most) : most;
@@ -103,7 +103,7 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   const long long tile = x.chunk_rows, in_tile = std::min(tile, (rows + seqs - 1) / seqs);
   const long long tiles = std::max((rows + tile - 1) / tile, seqs);
   const long long min_keys = std::max<long long>(256, 8 * in_tile);
-  x.chunk_splits = x.chunk ? pieces(tiles * p->Hkv, x.chunk_rows == 256 ? 256 : in_tile <= 16 ? 2048 : 512, min_keys) : 1;
+  x.chunk_splits = x.chunk ? pieces(tiles * p->Hkv, in_tile <= 16 ? 2048 : x.chunk_rows == 256 ? 256 : 512, min_keys) : 1;
   x.chunk_min = (int)(min_keys / tile_keys(p));
   x.few_splits = x.few ? pieces(seqs * p->Hkv, 2048, 256) : 1;
   x.few_min = 256 / (f32 ? 16 : 32);

@@ -767,29 +767,37 @@ __global__ void __launch_bounds__(256, 2) paged_few_kernel(PArgs a, int first_bl
   few_workgroup<D, E4M3, BY16, NQ>(a, first_block + block_id(), smem);
 }
 
-template <int D, bool E4M3, bool BY16>
+template <int D, bool E4M3, bool BY16, int NQ>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_both_kernel(PArgs a, int first_block) {
-  __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D> > kFewBytes<D, 2> ? kChunkBytes<D> : kFewBytes<D, 2>];
+  __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D> > kFewBytes<D, NQ> ? kChunkBytes<D> : kFewBytes<D, NQ>];
   __shared__ int flags[4];
   const int block = first_block + block_id();
   if (block < a.chunk_blocks)   // the long chains first: 62 us, the others first 72 (16 sequences of 1 to 600 rows, window 4096)
     chunk_workgroup<D, E4M3, BY16>(a, block, smem, flags);
   else
-    few_workgroup<D, E4M3, BY16, 2>(a, block - a.chunk_blocks, smem);
+    few_workgroup<D, E4M3, BY16, NQ>(a, block - a.chunk_blocks, smem);
 }
 
+template <int D, bool E4M3, bool BY16, int NQ>
+int launch_few(const PArgs& a, hipStream_t st) {
+  return launch_blocks(paged_few_kernel<D, E4M3, BY16, NQ>, a.B * a.Hkv * a.few.splits, 256, st, a);
+}
+template <int D, bool E4M3, bool BY16, int NQ>
+int launch_both(const PArgs& a, hipStream_t st) {
+  return launch_blocks(paged_both_kernel<D, E4M3, BY16, NQ>, a.chunk_blocks + a.B * a.Hkv * a.few.splits, 256, st, a);
+}
 template <int D, bool E4M3, bool BY16>
 int launch_t(const PArgs& a, int nq, hipStream_t st) {
-  const int few = a.B * a.Hkv * a.few.splits;
+  if (a.chunk_blocks == 0) return nq == 1 ? launch_few<D, E4M3, BY16, 1>(a, st) : launch_few<D, E4M3, BY16, 2>(a, st);
   if constexpr (D == 128 && BY16) {
-    if (a.chunk_blocks > 0 && a.chunk_rows == 256) {
+    if (a.chunk_rows == 256) {
       const int rc = launch_blocks(paged_long_kernel<E4M3>, a.chunk_blocks, 512, st, a);
-      return rc != 0 || a.few_rows == 0 ? rc : launch_blocks(paged_few_kernel<D, E4M3, BY16, 2>, few, 256, st, a);
+      if (rc != 0 || a.few_rows == 0) return rc;
+      return nq == 1 ? launch_few<D, E4M3, BY16, 1>(a, st) : launch_few<D, E4M3, BY16, 2>(a, st);
     }
   }
   if (a.few_rows == 0) return launch_blocks(paged_chunk_kernel<D, E4M3, BY16>, a.chunk_blocks, 256, st, a);
-  if (a.chunk_blocks > 0) return launch_blocks(paged_both_kernel<D, E4M3, BY16>, a.chunk_blocks + few, 256, st, a);
-  return nq == 1 ? launch_blocks(paged_few_kernel<D, E4M3, BY16, 1>, few, 256, st, a) : launch_blocks(paged_few_kernel<D, E4M3, BY16, 2>, few, 256, st, a);
+  return nq == 1 ? launch_both<D, E4M3, BY16, 1>(a, st) : launch_both<D, E4M3, BY16, 2>(a, st);
 }
 template <int D, bool E4M3>
 int launch_pages(const PArgs& a, int nq, hipStream_t st) {
