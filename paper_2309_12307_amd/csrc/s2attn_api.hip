@@ -236,12 +236,31 @@ bool dq_reuses_input(const s2attn_params* p) {
 
 // ---- window attention: one causal run of all tokens, no groups or shifts.
 struct WindowPlan {
+  bool small_fwd, small_bwd;   // the kernels for few rows
   int parts;
   s2::Win win;
   size_t rows, partial, far;   // bytes of the workspace: row terms, partial dk, dv of the parts, of the cut key tiles
 };
 
 constexpr int kMostSegments = 15, kMostCutTiles = 8;
+
+// Few rows go to the kernels that give a workgroup 32 of them (fp32: 16), by the tiles of 32 (64) rows of all heads.  us, these and
+// the others, four sinks, window 512:
+//   bf16, 256 tiles   H = 8, N = 1000          forward 12.7 and 19.8, backward 39 and 59
+//         320         H = 32, Hkv = 8, N = 300         11.3 and 11.4,          28 and 64 (window 128)
+//         512         H = 8, N = 2048                  23.7 and 20.0,          74 and 64
+//   fp32, 128 tiles   H = 16, N = 512, D = 128         23.7 and 45.9,          75 and 84
+//         160         H = 32, Hkv = 8, N = 300, D = 128  16.5 and 24.6,        58 and 74 (window 128)
+//         256         H = 4, N = 4096, D = 64 (128)    32 and 35 (58 and 57), 123 and 126 (239 and 175)
+//         768         H = 12, Hkv = 4, N = 4096, D = 64  81 and 78,           317 and 275
+void window_small(const s2attn_params* p, bool& fwd, bool& bwd) {
+  const bool f32 = p->dtype == S2ATTN_F32;
+  const int rows = f32 ? 64 : 32;
+  const long long tiles = (long long)p->B * p->H * ((p->N + rows - 1LL) / rows);
+  const bool built = f32 || p->D == 128;
+  fwd = built && tiles <= 256;
+  bwd = built && tiles <= (f32 ? 160 : 320);
+}
 
 // The first keys' dK/dV is cut where the sinks are few key tiles and their queries more than their windows': a
 // segment then is as long as the other workgroups' chains, or more where that would take over kMostSegments.  With more sink
@@ -251,7 +270,8 @@ WindowPlan window_plan(const s2attn_params* p, int window, int sinks, size_t ava
   WindowPlan x;
   std::memset(&x, 0, sizeof(x));
   const bool f32 = p->dtype == S2ATTN_F32;
-  const int KT = f32 ? 64 : 128, QT = f32 ? 32 : 64, r = p->H / p->Hkv;
+  window_small(p, x.small_fwd, x.small_bwd);
+  const int KT = x.small_bwd ? (f32 ? 16 : 32) : f32 ? 64 : 128, QT = x.small_bwd ? KT : f32 ? 32 : 64, r = p->H / p->Hkv;
   x.win.window = std::min(window, p->N);
   x.win.sinks = std::min(sinks, p->N);
   const int tiles = (x.win.sinks + KT - 1) / KT, all = (p->N + QT - 1) / QT;
@@ -556,7 +576,8 @@ int s2attn_window_fwd(const s2attn_params* p, int window, int sinks, void* strea
   s2::KArgs a = make_kargs(&local);
   a.ragged = 1;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  rc = p->dtype == S2ATTN_F32 ? s2::launch_window_fwd_f32(a, x.win, st) : s2::launch_window_fwd_bf16(a, x.win, st);
+  if (p->dtype == S2ATTN_F32) rc = x.small_fwd ? s2::launch_window_fwd_f32_small(a, x.win, st) : s2::launch_window_fwd_f32(a, x.win, st);
+  else rc = x.small_fwd ? s2::launch_window_fwd_small(a, x.win, st) : s2::launch_window_fwd_bf16(a, x.win, st);
   return rc == 0 ? S2ATTN_OK : S2ATTN_ERR_LAUNCH;
 }
 
@@ -577,14 +598,16 @@ int s2attn_window_bwd(const s2attn_params* p, int window, int sinks, void* strea
   x.win.partial = reinterpret_cast<float*>(ws + x.rows + x.partial);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (p->dtype == S2ATTN_F32) {
-    rc = s2::launch_window_bwd_f32(a, x.win, st);
+    rc = x.small_bwd ? s2::launch_window_bwd_f32_small(a, x.win, st) : s2::launch_window_bwd_f32(a, x.win, st);
+  } else if (x.small_bwd) {
+    rc = s2::launch_window_bwd_small(a, x.win, st);
   } else {
     rc = s2::launch_delta_bf16(a, st);
     if (rc == 0) rc = s2::launch_window_bwd_bf16(a, x.win, st);
   }
   // (the parts' sum leaves cut key tiles to the sum of their segments, which comes after it)
   if (rc == 0 && a.parts > 1) rc = s2::launch_combine_partials(a, p->dtype, st);
-  if (rc == 0 && x.win.sink_tiles > 0) rc = s2::launch_sink_combine(a, x.win, p->dtype, st);
+  if (rc == 0 && x.win.sink_tiles > 0) rc = s2::launch_sink_combine(a, x.win, p->dtype, x.small_bwd, st);
   return rc == 0 ? S2ATTN_OK : S2ATTN_ERR_LAUNCH;
 }
 

@@ -474,11 +474,12 @@ int launch_bwd_dkdv_bf16(const KArgs& a, hipStream_t st) {
 
 int launch_window_bwd_bf16(const KArgs& a, Win win, hipStream_t st) {
   if (a.D == 64) return launch_window_bwd_d64(a, win, st);
-  const int T = ragged_tiles(a, 128), n_seq = a.B * a.Hkv * a.parts;
-  const Grid kv = grid_of(T, n_seq, 1, 32), q = grid_of(T, a.B * a.H, a.r, 64);
-  win.n_main = kv.blocks;
-  const int rc = launch_blocks(window_dkdv_bf16_kernel, kv.blocks + n_seq * win.sink_tiles * win.n_seg, 512, st, a, T, kv.deal, win);
-  return rc != 0 ? rc : launch_blocks(window_dq_bf16_kernel, q.blocks, 256, st, a, T, q.deal, win);
+  const int tiles = ragged_tiles(a, 128), n_seq = a.B * a.Hkv * a.parts;
+  const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 32);
+  const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);
+  const WindowGrid q = window_grid_q(win, tiles, a.B * a.H, a.r, 64);
+  const int rc = launch_blocks(window_dkdv_bf16_kernel, n_kv, 512, st, a, kv.T, kv.grid.deal, win);
+  return rc != 0 ? rc : launch_blocks(window_dq_bf16_kernel, q.grid.blocks, 256, st, a, q.T, q.grid.deal, win);
 }
 
 int launch_bwd_dq_bf16(const KArgs& a, hipStream_t st) {

@@ -104,11 +104,15 @@ __device__ __forceinline__ void fwd64_workgroup(const KArgs& a, int T, const Dea
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
 
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int c = at.c, b = at.b, h = at.h;
-  int qt = T - 1 - rank;
   const int s = uni(shift_of_head(a, h));
   Run run;
   if (!run_of_tile(a, at.g, s, kOwn, qt, run)) return;
@@ -533,11 +537,15 @@ __device__ __forceinline__ void dq64_workgroup(const KArgs& a, int T, const Deal
   const int lane = tid & 63, w = uni(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
 
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int c = at.c, b = at.b, h = at.h;
-  int qt = T - 1 - rank;
   const int s = uni(shift_of_head(a, h));
   Run run;
   if (!run_of_tile(a, at.g, s, kOwn, qt, run)) return;
@@ -613,14 +621,14 @@ bwd_dq_d64_kernel(KArgs a, int T, Deal deal, int first_block) {
 
 // The same under a window, always in one launch.
 __global__ void __launch_bounds__(256, 2)
-window_bwd_d64_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, Win win, int first_block) {
+window_bwd_d64_kernel(KArgs a, int n_kv, int T_kv, Deal deal_kv, int T_q, Deal deal_q, Win win, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[4 * kTile];
   __shared__ __attribute__((aligned(1024))) RowTerms rows_s[2];
   const int block = first_block + block_id();
   if (block < n_kv)
-    dkdv64_workgroup<true>(a, T, deal_kv, block, thread_id(), smem, rows_s, win);
+    dkdv64_workgroup<true>(a, T_kv, deal_kv, block, thread_id(), smem, rows_s, win);
   else
-    dq64_workgroup<true>(a, T, deal_q, block - n_kv, thread_id(), smem, win);
+    dq64_workgroup<true>(a, T_q, deal_q, block - n_kv, thread_id(), smem, win);
 }
 
 // Both in one launch, dK/dV first: neither needs the other, and where they do not fill the chip their
@@ -643,18 +651,16 @@ int launch_fwd_d64(const KArgs& a, hipStream_t st) {
   return launch_blocks(fwd_d64_kernel, g.blocks, 256, st, a, T, g.deal);
 }
 
-int launch_window_fwd_d64(const KArgs& a, const Win& win, hipStream_t st) {
-  const int T = ragged_tiles(a, kOwn);
-  const Grid g = grid_of(T, a.B * a.H, a.r, 128);
-  return launch_blocks(window_fwd_d64_kernel, g.blocks, 256, st, a, T, g.deal, win);
+int launch_window_fwd_d64(const KArgs& a, Win win, hipStream_t st) {
+  const WindowGrid g = window_grid_q(win, ragged_tiles(a, kOwn), a.B * a.H, a.r, 128);
+  return launch_blocks(window_fwd_d64_kernel, g.grid.blocks, 256, st, a, g.T, g.grid.deal, win);
 }
 
 int launch_window_bwd_d64(const KArgs& a, Win win, hipStream_t st) {
-  const int T = ragged_tiles(a, kOwn), n_seq = a.B * a.Hkv * a.parts;
-  const Grid kv = grid_of(T, n_seq, 1, 64), q = grid_of(T, a.B * a.H, a.r, 64);
-  win.n_main = kv.blocks;
-  const int n_kv = pad_to(kv.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
-  return launch_blocks(window_bwd_d64_kernel, n_kv + q.blocks, 256, st, a, n_kv, T, kv.deal, q.deal, win);
+  const int tiles = ragged_tiles(a, kOwn), n_seq = a.B * a.Hkv * a.parts;
+  const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 64), q = window_grid_q(win, tiles, a.B * a.H, a.r, 64);
+  const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
+  return launch_blocks(window_bwd_d64_kernel, n_kv + q.grid.blocks, 256, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
 }
 
 int launch_bwd_dkdv_d64(const KArgs& a, hipStream_t st) {

@@ -130,11 +130,15 @@ __device__ __forceinline__ void dq_workgroup(const KArgs& a, int T, const Deal& 
   const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
 
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int gidx = at.g, c = at.c, b = at.b, h = at.h;
-  int qt = T - 1 - rank;
 
   const int s = uni(shift_of_head(a, h));
   Run run{gidx * a.G, a.G};                        // the causal run of this block (see the forward kernel)

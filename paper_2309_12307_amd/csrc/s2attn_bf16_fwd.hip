@@ -77,11 +77,15 @@ __device__ __forceinline__ void fwd_workgroup(const KArgs& a, int T, const Deal&
   // per query head and not per kv head: with one kv head and four groups the latter gave work to
   // four of the eight XCDs only (N = 8192, H = 32, G = 2048: forward 278 us,
   // 149 dealt out per query head; dQ 383 and 198).
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int gidx = at.g, c = at.c, b = at.b, h = at.h;
-  int qt = T - 1 - rank;
 
   const int s = uni(shift_of_head(a, h));
   // the causal run this block works in and the first row of the other block of a split
@@ -411,11 +415,11 @@ window_fwd_bf16_pp_kernel(KArgs a, int T, Deal deal, Win win) {
   __shared__ __attribute__((aligned(1024))) char smem[3 * 2 * kTileBytes];   // [stage][K,V]
   const int tid = thread_id(), lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g32 = lane >> 5, l32 = lane & 31;
-  int seq, rank;
-  if (!decode_block(block_id(), T, deal, seq, rank)) return;
+  int seq, qt;
+  if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block_id(), T, deal, seq, qt)) return;
   const HeadPos at = head_of_seq(a, seq);
   const int c = at.c, b = at.b, h = at.h;
-  const int i0 = uni((T - 1 - rank) * BM);
+  const int i0 = uni(qt * BM);
   const Run run{0, a.N};
   const int qw0 = i0 + w * 32, qrow = qw0 + l32;
   const KeyTiles kt = key_tiles<BN>(win.window, win.sinks, i0, i0 + BM - 1, a.N);
@@ -476,20 +480,18 @@ window_fwd_bf16_pp_kernel(KArgs a, int T, Deal deal, Win win) {
 
 }  // namespace
 
-int launch_window_fwd_bf16(const KArgs& a, const Win& win, hipStream_t st) {
+int launch_window_fwd_bf16(const KArgs& a, Win win, hipStream_t st) {
   if (a.D == 64) return launch_window_fwd_d64(a, win, st);
   // Eight waves only for long walks: of the tiles that 256 rows meet a wave's 32 need all but three or four, and one workgroup a
   // CU has nothing beside its first and last tile.  us, four waves and eight, N = 32768, H = 32, four sinks: window 1024 756
   // and 786, 2048 1252 and 1260, 4096 2193 and 2089, 8192 3833 and 3564; N = 4096 2048 131 and 127, 4096 146 and 137.
   if (win.window >= 4096) {
-    const int T = ragged_tiles(a, 256);
-    const Grid g = grid_of(T, a.B * a.H, a.r, 32);
-    hipLaunchKernelGGL(window_fwd_bf16_pp_kernel, dim3(g.blocks), dim3(512), 0, st, a, T, g.deal, win);
+    const WindowGrid g = window_grid_q(win, ragged_tiles(a, 256), a.B * a.H, a.r, 32);
+    hipLaunchKernelGGL(window_fwd_bf16_pp_kernel, dim3(g.grid.blocks), dim3(512), 0, st, a, g.T, g.grid.deal, win);
     return hipGetLastError() == hipSuccess ? 0 : -1;
   }
-  const int T = ragged_tiles(a, 128);
-  const Grid g = grid_of(T, a.B * a.H, a.r, 64);
-  return launch_blocks(window_fwd_bf16_kernel, g.blocks, 256, st, a, T, g.deal, win);
+  const WindowGrid g = window_grid_q(win, ragged_tiles(a, 128), a.B * a.H, a.r, 64);
+  return launch_blocks(window_fwd_bf16_kernel, g.grid.blocks, 256, st, a, g.T, g.grid.deal, win);
 }
 
 int launch_fwd_bf16(const KArgs& a, hipStream_t st) {

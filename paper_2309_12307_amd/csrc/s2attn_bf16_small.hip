@@ -188,18 +188,22 @@ __device__ __forceinline__ float diag_cols(f32x4 d, int lane) {
   return __shfl(x, 16 * (c16 >> 2) + c16);
 }
 
-__global__ void __launch_bounds__(64 * kWaves, 1) fwd_small_kernel(KArgs a, int T, Deal deal, int first_block) {
-  __shared__ __attribute__((aligned(1024))) char smem[kSmemFwd];
-  __shared__ float max_s[kWaves][kRows], sum_s[kWaves][kRows];
-  fetch_args(a, deal);
+// WINDOW: one run of all tokens, key tiles of the sinks and of the window.
+template <bool WINDOW>
+__device__ __forceinline__ void fwd_small_block(const KArgs& a, int T, const Deal& deal, int block, const Win& win, char* smem,
+                                                float (&max_s)[kWaves][kRows], float (&sum_s)[kWaves][kRows]) {
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, rank;
-  if (!decode_block(first_block + block_id(), T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int s = uni(shift_of_head(a, at.h));
   Run run;
-  int qt = T - 1 - rank;
   if (!run_of_tile(a, at.g, s, kRows, qt, run)) return;
   qt = uni(qt); run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = qt * kRows, qrow = i0 + c16;
@@ -211,7 +215,11 @@ __global__ void __launch_bounds__(64 * kWaves, 1) fwd_small_kernel(KArgs a, int 
   const char* base = smem + w * kRingBytes;
   bf16x8 qf[4][2];
   load_own(qf, a, a.q, a.sq, run, s, at.b, at.h, i0, lane);
-  ring.begin(a, run, s, w * kRows, 0, w <= qt);
+  KeyTiles tiles{};
+  if constexpr (WINDOW) tiles = key_tiles<kRows>(win.window, win.sinks, i0, i0 + kRows - 1, a.N);
+  auto tile = [&](int n) __attribute__((always_inline)) { return WINDOW ? tiles.tile(n) : n; };
+  const int last = WINDOW ? tiles.total - 1 : qt;   // the tile on the diagonal
+  ring.begin(a, run, s, tile(w) * kRows, 0, w <= last);
   ring.all_pairs();
 
   LaneOffsets16 lo;
@@ -223,9 +231,9 @@ __global__ void __launch_bounds__(64 * kWaves, 1) fwd_small_kernel(KArgs a, int 
   float m_run[2] = {-3.402823466e38f, -3.402823466e38f}, l_run[2] = {0.f, 0.f};
   arrived(qf);
   int stage = 0;
-  for (int jt = w; jt <= qt; jt += kWaves, stage ^= 1) {
+  for (int jt = w; jt <= last; jt += kWaves, stage ^= 1) {
     wait_tile();
-    ring.begin(a, run, s, (jt + kWaves) * kRows, stage ^ 1, jt + kWaves <= qt);
+    ring.begin(a, run, s, tile(jt + kWaves) * kRows, stage ^ 1, jt + kWaves <= last);
     const char* Ks = base + stage * 2 * kTileBytes;
     const char* Vs = Ks + kTileBytes;
     f32x4 sc[2][2] = {{zero4(), zero4()}, {zero4(), zero4()}};
@@ -239,7 +247,11 @@ __global__ void __launch_bounds__(64 * kWaves, 1) fwd_small_kernel(KArgs a, int 
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float x = sc[kb][qb][e] * c2;
-          if (jt == qt && 16 * kb + 4 * q4 + e > c16 + 16 * qb) x = -INFINITY;
+          if (jt == last && 16 * kb + 4 * q4 + e > c16 + 16 * qb) x = -INFINITY;
+          if constexpr (WINDOW) {
+            const int key = tile(jt) * kRows + 16 * kb + 4 * q4 + e;
+            if ((qrow + 16 * qb - key >= win.window) & (key >= win.sinks)) x = -INFINITY;
+          }
           sc[kb][qb][e] = x;
           mx = fmaxf(mx, x);
         }
@@ -297,12 +309,31 @@ __global__ void __launch_bounds__(64 * kWaves, 1) fwd_small_kernel(KArgs a, int 
   }
 }
 
+__global__ void __launch_bounds__(64 * kWaves, 1) fwd_small_kernel(KArgs a, int T, Deal deal, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[kSmemFwd];
+  __shared__ float max_s[kWaves][kRows], sum_s[kWaves][kRows];
+  fetch_args(a, deal);
+  fwd_small_block<false>(a, T, deal, first_block + block_id(), Win{}, smem, max_s, sum_s);
+}
+
+__global__ void __launch_bounds__(64 * kWaves, 1) window_fwd_small_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[kSmemFwd];
+  __shared__ float max_s[kWaves][kRows], sum_s[kWaves][kRows];
+  fwd_small_block<true>(a, T, deal, first_block + block_id(), win, smem, max_s, sum_s);
+}
+
 // dK/dV of 32 keys; the waves share out the query tiles of all query heads of the part.
-__device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int block, int T, const Deal& deal) {
+// WINDOW: those that meet the keys' windows (query_tiles); dQ the key tiles of the sinks and of the window.
+template <bool WINDOW>
+__device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int block, int T, const Deal& deal, const Win& win) {
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, kt;
-  if (!decode_block(block, T, deal, seq, kt)) return;
+  int seq, kt, segment = 0;
+  if constexpr (WINDOW) {
+    if (!decode_window(win, block, T, deal, seq, kt, segment)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, kt)) return;
+  }
   const KvPos at = kv_of_seq(a, seq);
   int h_lo, nheads, s;
   part_heads(a, at.c, at.part, h_lo, nheads, s);
@@ -310,7 +341,14 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
   if (!run_of_tile(a, at.g, s, kRows, kt, run)) return;
   kt = uni(kt); run.p0 = uni(run.p0); run.len = uni(run.len);
   const int j0 = kt * kRows, key = j0 + c16;
-  const int nq = uni((run.len - 1) / kRows) - kt + 1;   // query tiles of a head, from the diagonal on
+  int it0 = 0;                                    // query tiles [it0, it0 + nq) of a head, counted from the diagonal
+  int nq = uni((run.len - 1) / kRows) - kt + 1;
+  if constexpr (WINDOW) {
+    const QueryTiles x = query_tiles<kRows, kRows>(win, a.N, kt, segment);
+    it0 = uni(x.lo);
+    nq = uni(x.hi - x.lo);
+    if (nq <= 0) return;                          // no such segment
+  }
   const float c2 = a.scale_log2;
 
   Ring ring;
@@ -320,7 +358,7 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
   float lse[2];
   // O and lse of tile `it` from the diagonal of head h_lo + hh
   auto load_rows = [&](int hh, int it) __attribute__((always_inline)) {
-    const int h = h_lo + hh, q0 = j0 + it * kRows;
+    const int h = h_lo + hh, q0 = j0 + (it0 + it) * kRows;
     load_own(of, a, a.o, a.so, run, s, at.b, h, q0, lane);
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb)
@@ -353,7 +391,7 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
       asm volatile("" : "+v"(lse[0]), "+v"(lse[1]));
     }
     if (more) ring.head(a.q, a.sq, h_lo + hn, a.dout, a.so, h_lo + hn, at.b);
-    ring.begin(a, run, s, j0 + in * kRows, stage ^ 1, more);
+    ring.begin(a, run, s, j0 + (it0 + in) * kRows, stage ^ 1, more);
     if (!cur) ring.all_pairs();
     bf16x8 gf[4][2];
     f32x4 delta[2], lse2[2];
@@ -385,7 +423,8 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
           for (int cb = 0; cb < 2; ++cb) dp[rb][cb] = mfma16(gf[k][rb], vf[k][cb], dp[rb][cb]);
         ring.pair(4 + k);
       }
-      const bool masked = diagonal || q0 + kRows > run.len;
+      const bool masked = diagonal || q0 + kRows > run.len ||
+                          (WINDOW && q0 + kRows - 1 - j0 >= win.window && j0 + kRows - 1 >= win.sinks);
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
@@ -395,6 +434,7 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
           for (int cb = 0; cb < 2; ++cb) {
             float p = __builtin_amdgcn_exp2f(fmaf(sc[rb][cb][e], c2, -lse2[rb][e]));
             if (masked && (key + 16 * cb > row || row >= run.len)) p = 0.f;
+            if (WINDOW && masked && (row - key - 16 * cb >= win.window) & (key + 16 * cb >= win.sinks)) p = 0.f;
             sc[rb][cb][e] = p;
             dp[rb][cb][e] *= p;
           }
@@ -406,8 +446,8 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
     }
     if (!more) break;
     cur = true;
-    diagonal = in == 0;
-    q0 = j0 + in * kRows;
+    diagonal = it0 + in == 0;
+    q0 = j0 + (it0 + in) * kRows;
     stage ^= 1;
     in += kWaves;
     settle(hn, in);
@@ -428,7 +468,14 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
     f32x4 x[2], y[2];
     sum_blocks(x, blocks, row, c, scale);
     sum_blocks(y, dv_blocks, row, c, one);
-    if (a.dkv_partial) {   // contiguous fp32 partial of this part, summed by the combine pass
+    if (WINDOW && kt < win.sink_tiles) {
+      f32x4* dst = reinterpret_cast<f32x4*>(far_row(win, a, 0, at.part, segment, at.b, at.c, t, kRows) + 8 * c);
+      dst[0] = x[0];
+      dst[1] = x[1];
+      dst = reinterpret_cast<f32x4*>(far_row(win, a, 1, at.part, segment, at.b, at.c, t, kRows) + 8 * c);
+      dst[0] = y[0];
+      dst[1] = y[1];
+    } else if (a.dkv_partial) {   // contiguous fp32 partial of this part, summed by the combine pass
       f32x4* dst = reinterpret_cast<f32x4*>(a.dkv_partial + at.part * elems + ((size_t)((size_t)at.b * a.N + t) * a.Hkv + at.c) * 128 + 8 * c);
       dst[0] = x[0];
       dst[1] = x[1];
@@ -443,15 +490,20 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, char* smem, int
 }
 
 // dQ of 32 query rows; the waves share out the key tiles.
-__device__ __forceinline__ void dq_small_block(const KArgs& a, char* smem, int block, int T, const Deal& deal) {
+template <bool WINDOW>
+__device__ __forceinline__ void dq_small_block(const KArgs& a, char* smem, int block, int T, const Deal& deal, const Win& win) {
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int s = uni(shift_of_head(a, at.h));
   Run run;
-  int qt = T - 1 - rank;
   if (!run_of_tile(a, at.g, s, kRows, qt, run)) return;
   qt = uni(qt); run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = qt * kRows;
@@ -461,6 +513,10 @@ __device__ __forceinline__ void dq_small_block(const KArgs& a, char* smem, int b
   ring.init(a.sk, a.sv, lds_addr(smem) + w * kRingBytes, lane);
   ring.head(a.k, a.sk, at.c, a.v, a.sv, at.c, at.b);
   const char* base = smem + w * kRingBytes;
+  KeyTiles tiles{};
+  if constexpr (WINDOW) tiles = key_tiles<kRows>(win.window, win.sinks, i0, i0 + kRows - 1, a.N);
+  auto tile = [&](int n) __attribute__((always_inline)) { return WINDOW ? tiles.tile(n) : n; };
+  const int last = WINDOW ? tiles.total - 1 : qt;   // the tile on the diagonal
   bf16x8 qf[4][2], gf[4][2];
   float delta[2], lse2[2];
   {
@@ -468,7 +524,7 @@ __device__ __forceinline__ void dq_small_block(const KArgs& a, char* smem, int b
     load_own(gf, a, a.dout, a.so, run, s, at.b, at.h, i0, lane);
     load_own(of, a, a.o, a.so, run, s, at.b, at.h, i0, lane);
     load_own(qf, a, a.q, a.sq, run, s, at.b, at.h, i0, lane);
-    ring.begin(a, run, s, w * kRows, 0, w <= qt);
+    ring.begin(a, run, s, tile(w) * kRows, 0, w <= last);
     ring.all_pairs();
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -484,9 +540,9 @@ __device__ __forceinline__ void dq_small_block(const KArgs& a, char* smem, int b
   f32x4 dq[8][2];
   zero(dq);
   int stage = 0;
-  for (int jt = w; jt <= qt; jt += kWaves, stage ^= 1) {
+  for (int jt = w; jt <= last; jt += kWaves, stage ^= 1) {
     wait_tile();
-    ring.begin(a, run, s, (jt + kWaves) * kRows, stage ^ 1, jt + kWaves <= qt);
+    ring.begin(a, run, s, tile(jt + kWaves) * kRows, stage ^ 1, jt + kWaves <= last);
     const char* Ks = base + stage * 2 * kTileBytes;
     const char* Vs = Ks + kTileBytes;
     f32x4 sc[2][2] = {{zero4(), zero4()}, {zero4(), zero4()}}, dp[2][2] = {{zero4(), zero4()}, {zero4(), zero4()}};
@@ -500,7 +556,11 @@ __device__ __forceinline__ void dq_small_block(const KArgs& a, char* smem, int b
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float p = __builtin_amdgcn_exp2f(fmaf(sc[kb][qb][e], c2, -lse2[qb]));
-          if (jt == qt && 16 * kb + 4 * q4 + e > c16 + 16 * qb) p = 0.f;
+          if (jt == last && 16 * kb + 4 * q4 + e > c16 + 16 * qb) p = 0.f;
+          if constexpr (WINDOW) {
+            const int key = tile(jt) * kRows + 16 * kb + 4 * q4 + e;
+            if ((i0 + c16 + 16 * qb - key >= win.window) & (key >= win.sinks)) p = 0.f;
+          }
           dp[kb][qb][e] = p * (dp[kb][qb][e] - delta[qb]);
         }
       ds[qb] = pack8(dp[0][qb], dp[1][qb]);
@@ -529,9 +589,19 @@ bwd_small_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, int first_
   fetch_args(a, deal_q);
   const int block = first_block + block_id();
   if (block < n_kv)
-    dkdv_small_block(a, smem, block, T, deal_kv);
+    dkdv_small_block<false>(a, smem, block, T, deal_kv, Win{});
   else
-    dq_small_block(a, smem, block - n_kv, T, deal_q);
+    dq_small_block<false>(a, smem, block - n_kv, T, deal_q, Win{});
+}
+
+__global__ void __launch_bounds__(64 * kWaves, 1)
+window_bwd_small_kernel(KArgs a, int n_kv, int T_kv, Deal deal_kv, int T_q, Deal deal_q, Win win, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[kSmemBwd];
+  const int block = first_block + block_id();
+  if (block < n_kv)
+    dkdv_small_block<true>(a, smem, block, T_kv, deal_kv, win);
+  else
+    dq_small_block<true>(a, smem, block - n_kv, T_q, deal_q, win);
 }
 
 }  // namespace
@@ -578,6 +648,18 @@ int launch_fwd_small(const KArgs& a, hipStream_t st) {
   const int T = ragged_tiles(a, kRows);
   const Grid g = grid_of(T, a.B * a.H * a.NG, a.r, 32);
   return launch_blocks(fwd_small_kernel, g.blocks, 64 * kWaves, st, a, T, g.deal);
+}
+
+int launch_window_fwd_small(const KArgs& a, Win win, hipStream_t st) {
+  const WindowGrid g = window_grid_q(win, ragged_tiles(a, kRows), a.B * a.H, a.r, 32);
+  return launch_blocks(window_fwd_small_kernel, g.grid.blocks, 64 * kWaves, st, a, g.T, g.grid.deal, win);
+}
+
+int launch_window_bwd_small(const KArgs& a, Win win, hipStream_t st) {
+  const int tiles = ragged_tiles(a, kRows), n_seq = a.B * a.Hkv * a.parts;
+  const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 32), q = window_grid_q(win, tiles, a.B * a.H, a.r, 32);
+  const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
+  return launch_blocks(window_bwd_small_kernel, n_kv + q.grid.blocks, 64 * kWaves, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
 }
 
 int launch_bwd_small(const KArgs& a, bool dq_last, hipStream_t st) {

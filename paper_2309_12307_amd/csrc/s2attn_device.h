@@ -212,9 +212,23 @@ struct Win {
   int window, sinks;
   int sink_tiles, n_seg, seg_tiles;   // key tiles that are cut (0: none, their workgroups take all queries), segments but 0
   int n_main;                         // blocks of segment 0; those of the others follow
+  int tiles;                          // row tiles of a sequence; the grids deal out its `cut` stretches as sequences of their
+  int cut_q, cut_kv;                  // own (forward and dQ; dK/dV)
   Div by_far, by_seg;                 // sink_tiles * n_seg, n_seg
+  Div by_cut_q, by_cut_kv;
   float* partial;
 };
+
+// Block -> (sequence, row tile): decode_block over stretches of T tiles, the last of a stretch first (DOWN: forward and dQ, whose
+// first tiles of a sequence see the fewest keys) or the first (dK/dV).
+template <bool DOWN>
+__device__ __forceinline__ bool decode_stretch(const Win& win, int cut, const Div& by_cut, int block, int T, const Deal& deal, int& seq, int& tile) {
+  int x, rank;
+  if (!decode_block(block, T, deal, x, rank)) return false;
+  seq = quot(x, by_cut);
+  tile = (x - seq * cut) * T + (DOWN ? T - 1 - rank : rank);
+  return tile < win.tiles;
+}
 
 // Query tiles [lo, hi) of QT rows, counted from key j0 on, of key tile jt = j0 / KT.
 struct QueryTiles {
@@ -232,13 +246,13 @@ __device__ __forceinline__ QueryTiles query_tiles(const Win& win, int N, int jt,
 // Block -> (sequence, key tile, segment) of dK/dV.
 __device__ __forceinline__ bool decode_window(const Win& win, int block, int T, const Deal& deal, int& seq, int& jt, int& segment) {
   segment = 0;
-  if (block < win.n_main) return decode_block(block, T, deal, seq, jt);
+  if (block < win.n_main) return decode_stretch<false>(win, win.cut_kv, win.by_cut_kv, block, T, deal, seq, jt);
   const int far = block - win.n_main;
   seq = quot(far, win.by_far);
   const int x = far - seq * win.sink_tiles * win.n_seg;
   jt = quot(x, win.by_seg);
   segment = 1 + x - jt * win.n_seg;
-  return seq < deal.n_seq;
+  return seq * win.cut_kv < deal.n_seq;
 }
 
 // Row of the partial dk (which = 0) or dv (1) of a segment.

@@ -49,12 +49,16 @@ __device__ __forceinline__ void fwd_f32_workgroup(const KArgs& a, int T, const D
   using L = Lanes<D>;
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int s = uni(shift_of_head(a, at.h));
   Run run;
-  int qt = T - 1 - rank;
   if (!run_of_tile(a, at.g, s, kWgRows, qt, run)) return;
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = uni(qt * kWgRows);
@@ -313,12 +317,16 @@ __device__ __forceinline__ void bwd_dq_block(const KArgs& a, char* smem, int blo
   using L = Lanes<D>;
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int s = uni(shift_of_head(a, at.h));
   Run run;
-  int qt = T - 1 - rank;
   if (!run_of_tile(a, at.g, s, kWgRows, qt, run)) return;
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = uni(qt * kWgRows);
@@ -405,14 +413,14 @@ bwd_f32_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, int first_bl
 
 template <int D>
 __global__ void __launch_bounds__(256, 2)
-window_bwd_f32_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, Win win, int first_block) {
+window_bwd_f32_kernel(KArgs a, int n_kv, int T_kv, Deal deal_kv, int T_q, Deal deal_q, Win win, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[4 * Lanes<D>::kTileBytes];
   __shared__ __attribute__((aligned(16))) float rows_s[2 * 2 * kTile];
   const int block = first_block + block_id();
   if (block < n_kv)
-    bwd_dkdv_block<D, true>(a, smem, rows_s, block, T, deal_kv, win);
+    bwd_dkdv_block<D, true>(a, smem, rows_s, block, T_kv, deal_kv, win);
   else
-    bwd_dq_block<D, true>(a, smem, block - n_kv, T, deal_q, win);
+    bwd_dq_block<D, true>(a, smem, block - n_kv, T_q, deal_q, win);
 }
 
 template <int D>
@@ -423,19 +431,17 @@ int launch_fwd_t(const KArgs& a, hipStream_t st) {
 }
 
 template <int D>
-int launch_window_fwd_t(const KArgs& a, const Win& win, hipStream_t st) {
-  const int T = ragged_tiles(a, kWgRows);
-  const Grid g = grid_of(T, a.B * a.H, a.r, 64);
-  return launch_blocks(window_fwd_f32_kernel<D>, g.blocks, 256, st, a, T, g.deal, win);
+int launch_window_fwd_t(const KArgs& a, Win win, hipStream_t st) {
+  const WindowGrid g = window_grid_q(win, ragged_tiles(a, kWgRows), a.B * a.H, a.r, 64);
+  return launch_blocks(window_fwd_f32_kernel<D>, g.grid.blocks, 256, st, a, g.T, g.grid.deal, win);
 }
 
 template <int D>
 int launch_window_bwd_t(const KArgs& a, Win win, hipStream_t st) {
-  const int T = ragged_tiles(a, kWgRows), n_seq = a.B * a.Hkv * a.parts;
-  const Grid kv = grid_of(T, n_seq, 1, 64), q = grid_of(T, a.B * a.H, a.r, 64);
-  win.n_main = kv.blocks;
-  const int n_kv = pad_to(kv.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
-  return launch_blocks(window_bwd_f32_kernel<D>, n_kv + q.blocks, 256, st, a, n_kv, T, kv.deal, q.deal, win);
+  const int tiles = ragged_tiles(a, kWgRows), n_seq = a.B * a.Hkv * a.parts;
+  const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 64), q = window_grid_q(win, tiles, a.B * a.H, a.r, 64);
+  const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
+  return launch_blocks(window_bwd_f32_kernel<D>, n_kv + q.grid.blocks, 256, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
 }
 
 template <int D>
@@ -481,11 +487,11 @@ bool small_bwd(const KArgs& a) {
 
 }  // namespace
 
-int launch_window_fwd_f32(const KArgs& a, const Win& win, hipStream_t st) {
+int launch_window_fwd_f32(const KArgs& a, Win win, hipStream_t st) {
   return a.D == 64 ? launch_window_fwd_t<64>(a, win, st) : launch_window_fwd_t<128>(a, win, st);
 }
 
-int launch_window_bwd_f32(const KArgs& a, const Win& win, hipStream_t st) {
+int launch_window_bwd_f32(const KArgs& a, Win win, hipStream_t st) {
   return a.D == 64 ? launch_window_bwd_t<64>(a, win, st) : launch_window_bwd_t<128>(a, win, st);
 }
 

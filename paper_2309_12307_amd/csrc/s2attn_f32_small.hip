@@ -94,20 +94,22 @@ __device__ __forceinline__ f32x4 sum_blocks(const float* blocks, int f, const fl
   return x;
 }
 
-template <int D>
-__global__ void __launch_bounds__(64 * kWaves, 2) fwd_f32_small_kernel(KArgs a, int T, Deal deal, int first_block) {
-  __shared__ __attribute__((aligned(16))) float blocks[kWaves * kBlockFloats<D>];
-  __shared__ float max_s[kWaves][kRows], sum_s[kWaves][kRows];
-  fetch_args(a, deal);
-
+// WINDOW: one run of all tokens, key tiles of the sinks and of the window.
+template <int D, bool WINDOW>
+__device__ __forceinline__ void fwd_small_block(const KArgs& a, int T, const Deal& deal, int block, const Win& win, float* blocks,
+                                                float (&max_s)[kWaves][kRows], float (&sum_s)[kWaves][kRows]) {
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, rank;
-  if (!decode_block(first_block + block_id(), T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int s = uni(shift_of_head(a, at.h));
   Run run;
-  int qt = T - 1 - rank;
   if (!run_of_tile(a, at.g, s, kRows, qt, run)) return;
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = uni(qt * kRows), qrow = i0 + c16;
@@ -121,23 +123,30 @@ __global__ void __launch_bounds__(64 * kWaves, 2) fwd_f32_small_kernel(KArgs a, 
   auto load_v = [&](int jt) __attribute__((always_inline)) {
     load_tr<D>(vf, a, a.v, a.sv, run, s, at.b, at.c, jt * kRows, c16, q4);
   };
-  const int last = i0 / kRows;   // the tile on the diagonal
+  KeyTiles tiles{};
+  if constexpr (WINDOW) tiles = key_tiles<kRows>(win.window, win.sinks, i0, i0 + kRows - 1, a.N);
+  auto tile = [&](int n) __attribute__((always_inline)) { return WINDOW ? tiles.tile(n) : n; };
+  const int last = WINDOW ? tiles.total - 1 : i0 / kRows;   // the tile on the diagonal
   if (w <= last) {
-    load_k(w);
+    load_k(tile(w));
     load_rm<D>(qf, static_cast<const float*>(a.q) + row_off(a.sq, at.b, tok, at.h), q4);
-    load_v(w);
+    load_v(tile(w));
   }
   zero<D>(o);
   float m_run = -FLT_MAX, l_run = 0.f;   // as in fwd_f32_kernel
   for (int jt = w; jt <= last; jt += kWaves) {
     const bool more = jt + kWaves <= last;
     f32x4 sc = scores<D>(kf, qf, f32x4{0.f, 0.f, 0.f, 0.f});
-    if (more) load_k(jt + kWaves);
+    if (more) load_k(tile(jt + kWaves));
     float mx = -INFINITY;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       sc[v] *= c2;
       if (jt == last && 4 * q4 + v > c16) sc[v] = -INFINITY;
+      if constexpr (WINDOW) {
+        const int key = tile(jt) * kRows + 4 * q4 + v;
+        if ((qrow - key >= win.window) & (key >= win.sinks)) sc[v] = -INFINITY;
+      }
       mx = fmaxf(mx, sc[v]);
     }
     mx = max_cols(mx);
@@ -157,7 +166,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) fwd_f32_small_kernel(KArgs a, 
       l_run += sc[v];
     }
     accumulate<D>(o, vf, sc);
-    if (more) load_v(jt + kWaves);
+    if (more) load_v(tile(jt + kWaves));
   }
   l_run = sum_cols(l_run);
   store_row<D>(blocks + w * kBlockFloats<D> + c16 * (D + 4), o, 1.f, q4);
@@ -186,16 +195,36 @@ __global__ void __launch_bounds__(64 * kWaves, 2) fwd_f32_small_kernel(KArgs a, 
   }
 }
 
+template <int D>
+__global__ void __launch_bounds__(64 * kWaves, 2) fwd_f32_small_kernel(KArgs a, int T, Deal deal, int first_block) {
+  __shared__ __attribute__((aligned(16))) float blocks[kWaves * kBlockFloats<D>];
+  __shared__ float max_s[kWaves][kRows], sum_s[kWaves][kRows];
+  fetch_args(a, deal);
+  fwd_small_block<D, false>(a, T, deal, first_block + block_id(), Win{}, blocks, max_s, sum_s);
+}
+
+template <int D>
+__global__ void __launch_bounds__(64 * kWaves, 2) window_fwd_f32_small_kernel(KArgs a, int T, Deal deal, Win win, int first_block) {
+  __shared__ __attribute__((aligned(16))) float blocks[kWaves * kBlockFloats<D>];
+  __shared__ float max_s[kWaves][kRows], sum_s[kWaves][kRows];
+  fwd_small_block<D, true>(a, T, deal, first_block + block_id(), win, blocks, max_s, sum_s);
+}
+
 // ---------------------------------------------------------------------------
 // Backward, one launch as in bwd_f32_kernel.  dK/dV: 16 keys; the waves share out the tiles of 16 query
 // rows, all query heads of the part.  dQ: 16 query rows; the waves share out the key tiles.
 // ---------------------------------------------------------------------------
-template <int D>
-__device__ __forceinline__ void dkdv_small_block(const KArgs& a, float* blocks, int block, int T, const Deal& deal) {
+// WINDOW: the query tiles that meet the keys' windows (query_tiles); dQ the key tiles of the sinks and of the window.
+template <int D, bool WINDOW>
+__device__ __forceinline__ void dkdv_small_block(const KArgs& a, float* blocks, int block, int T, const Deal& deal, const Win& win) {
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, kt;
-  if (!decode_block(block, T, deal, seq, kt)) return;
+  int seq, kt, segment = 0;
+  if constexpr (WINDOW) {
+    if (!decode_window(win, block, T, deal, seq, kt, segment)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, kt)) return;
+  }
   const KvPos at = kv_of_seq(a, seq);
   int h_lo, nheads, s;
   part_heads(a, at.c, at.part, h_lo, nheads, s);
@@ -203,7 +232,14 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, float* blocks, 
   if (!run_of_tile(a, at.g, s, kRows, kt, run)) return;
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int j0 = uni(kt * kRows), key = j0 + c16;
-  const int nq = uni((run.len - 1) / kRows) - j0 / kRows + 1;   // query tiles of a head, from the diagonal on
+  int it0 = 0;                                           // query tiles [it0, it0 + nq) of a head, counted from the diagonal
+  int nq = uni((run.len - 1) / kRows) - j0 / kRows + 1;
+  if constexpr (WINDOW) {
+    const QueryTiles x = query_tiles<kRows, kRows>(win, a.N, kt, segment);
+    it0 = uni(x.lo);
+    nq = uni(x.hi - x.lo);
+    if (nq <= 0) return;                                 // no such segment
+  }
   const float c2 = a.scale_log2;
 
   const int tok = run_token(a, run, j0 + c16, s);
@@ -211,7 +247,7 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, float* blocks, 
   float lse = 0.f;
   // first row of the it-th query tile: from the end of the run to the diagonal, so that the large
   // probabilities are added last
-  auto first_row = [&](int it) __attribute__((always_inline)) { return j0 + (nq - 1 - it) * kRows; };
+  auto first_row = [&](int it) __attribute__((always_inline)) { return j0 + (it0 + nq - 1 - it) * kRows; };
   auto load_rows = [&](int h, int it) __attribute__((always_inline)) {
     const int t = run_token(a, run, first_row(it) + c16, s);
     load_rm<D>(qf, static_cast<const float*>(a.q) + row_off(a.sq, at.b, t, h), q4);
@@ -267,6 +303,7 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, float* blocks, 
       const int i = q0 + 4 * q4 + v;
       float p = exp2f(fmaf(sc[v], c2, -__shfl(l, 4 * q4 + v)));
       if (key > i || i >= run.len) p = 0.f;
+      if (WINDOW && (i - key >= win.window) & (key >= win.sinks)) p = 0.f;
       sc[v] = p;
       dp[v] = (dp[v] - __shfl(delta, 4 * q4 + v)) * p;
     }
@@ -292,7 +329,10 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, float* blocks, 
     if (j0 + row >= run.len) break;
     const int t = token_of(run.p0 + j0 + row, s, a.N);
     const f32x4 x = sum_blocks<D>(blocks, f, one), y = sum_blocks<D>(dv_blocks, f, one);
-    if (a.dkv_partial) {   // contiguous fp32 partial of this part, summed by the combine pass
+    if (WINDOW && kt < win.sink_tiles) {
+      *reinterpret_cast<f32x4*>(far_row(win, a, 0, at.part, segment, at.b, at.c, t, kRows) + col) = x;
+      *reinterpret_cast<f32x4*>(far_row(win, a, 1, at.part, segment, at.b, at.c, t, kRows) + col) = y;
+    } else if (a.dkv_partial) {   // contiguous fp32 partial of this part, summed by the combine pass
       float* dst = a.dkv_partial + at.part * elems + ((size_t)((size_t)at.b * a.N + t) * a.Hkv + at.c) * D + col;
       *reinterpret_cast<f32x4*>(dst) = x;
       *reinterpret_cast<f32x4*>(dst + a.parts * elems) = y;
@@ -303,16 +343,20 @@ __device__ __forceinline__ void dkdv_small_block(const KArgs& a, float* blocks, 
   }
 }
 
-template <int D>
-__device__ __forceinline__ void dq_small_block(const KArgs& a, float* blocks, int block, int T, const Deal& deal) {
+template <int D, bool WINDOW>
+__device__ __forceinline__ void dq_small_block(const KArgs& a, float* blocks, int block, int T, const Deal& deal, const Win& win) {
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  int seq, rank;
-  if (!decode_block(block, T, deal, seq, rank)) return;
+  int seq, rank, qt;
+  if constexpr (WINDOW) {
+    if (!decode_stretch<true>(win, win.cut_q, win.by_cut_q, block, T, deal, seq, qt)) return;
+  } else {
+    if (!decode_block(block, T, deal, seq, rank)) return;
+    qt = T - 1 - rank;
+  }
   const HeadPos at = head_of_seq(a, seq);
   const int s = uni(shift_of_head(a, at.h));
   Run run;
-  int qt = T - 1 - rank;
   if (!run_of_tile(a, at.g, s, kRows, qt, run)) return;
   run.p0 = uni(run.p0); run.len = uni(run.len);
   const int i0 = uni(qt * kRows), qrow = i0 + c16;
@@ -329,17 +373,20 @@ __device__ __forceinline__ void dq_small_block(const KArgs& a, float* blocks, in
   auto load_kt = [&](int jt) __attribute__((always_inline)) {
     load_tr<D>(kt, a, a.k, a.sk, run, s, at.b, at.c, jt * kRows, c16, q4);
   };
-  const int last = i0 / kRows;
+  KeyTiles tiles{};
+  if constexpr (WINDOW) tiles = key_tiles<kRows>(win.window, win.sinks, i0, i0 + kRows - 1, a.N);
+  auto tile = [&](int n) __attribute__((always_inline)) { return WINDOW ? tiles.tile(n) : n; };
+  const int last = WINDOW ? tiles.total - 1 : i0 / kRows;
   float delta = 0.f, lse2 = 0.f;
   if (w <= last) {
-    load_k(w);
+    load_k(tile(w));
     load_rm<D>(qf, static_cast<const float*>(a.q) + row_off(a.sq, at.b, tok, at.h), q4);
-    load_v(w);
+    load_v(tile(w));
     load_rm<D>(gf, static_cast<const float*>(a.dout) + row_off(a.so, at.b, tok, at.h), q4);
     f32x4 of[D / 16];
     load_rm<D>(of, static_cast<const float*>(a.o) + row_off(a.so, at.b, tok, at.h), q4);
     lse2 = a.lse[((size_t)at.b * a.H + at.h) * a.N + tok] * kLog2e;
-    load_kt(w);
+    load_kt(tile(w));
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -350,17 +397,21 @@ __device__ __forceinline__ void dq_small_block(const KArgs& a, float* blocks, in
   for (int jt = w; jt <= last; jt += kWaves) {
     const bool more = jt + kWaves <= last;
     f32x4 sc = scores<D>(kf, qf, f32x4{0.f, 0.f, 0.f, 0.f});
-    if (more) load_k(jt + kWaves);
+    if (more) load_k(tile(jt + kWaves));
     f32x4 dp = scores<D>(vf, gf, f32x4{-delta, -delta, -delta, -delta});
-    if (more) load_v(jt + kWaves);
+    if (more) load_v(tile(jt + kWaves));
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       float p = exp2f(fmaf(sc[v], c2, -lse2));
       if (jt == last && 4 * q4 + v > c16) p = 0.f;
+      if constexpr (WINDOW) {
+        const int key = tile(jt) * kRows + 4 * q4 + v;
+        if ((qrow - key >= win.window) & (key >= win.sinks)) p = 0.f;
+      }
       dp[v] *= p;
     }
     accumulate<D>(dq, kt, dp);
-    if (more) load_kt(jt + kWaves);
+    if (more) load_kt(tile(jt + kWaves));
   }
   store_row<D>(blocks + w * kBlockFloats<D> + c16 * (D + 4), dq, a.scale, q4);
   __syncthreads();
@@ -384,9 +435,34 @@ bwd_f32_small_kernel(KArgs a, int n_kv, int T, Deal deal_kv, Deal deal_q, int fi
   fetch_args(a, deal_q);
   const int block = first_block + block_id();
   if (block < n_kv)
-    dkdv_small_block<D>(a, blocks, block, T, deal_kv);
+    dkdv_small_block<D, false>(a, blocks, block, T, deal_kv, Win{});
   else
-    dq_small_block<D>(a, blocks, block - n_kv, T, deal_q);
+    dq_small_block<D, false>(a, blocks, block - n_kv, T, deal_q, Win{});
+}
+
+template <int D>
+__global__ void __launch_bounds__(64 * kWaves, 2)
+window_bwd_f32_small_kernel(KArgs a, int n_kv, int T_kv, Deal deal_kv, int T_q, Deal deal_q, Win win, int first_block) {
+  __shared__ __attribute__((aligned(16))) float blocks[2 * kWaves * kBlockFloats<D>];
+  const int block = first_block + block_id();
+  if (block < n_kv)
+    dkdv_small_block<D, true>(a, blocks, block, T_kv, deal_kv, win);
+  else
+    dq_small_block<D, true>(a, blocks, block - n_kv, T_q, deal_q, win);
+}
+
+template <int D>
+int launch_window_fwd_t(const KArgs& a, Win win, hipStream_t st) {
+  const WindowGrid g = window_grid_q(win, ragged_tiles(a, kRows), a.B * a.H, a.r, 64);
+  return launch_blocks(window_fwd_f32_small_kernel<D>, g.grid.blocks, 64 * kWaves, st, a, g.T, g.grid.deal, win);
+}
+
+template <int D>
+int launch_window_bwd_t(const KArgs& a, Win win, hipStream_t st) {
+  const int tiles = ragged_tiles(a, kRows), n_seq = a.B * a.Hkv * a.parts;
+  const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 64), q = window_grid_q(win, tiles, a.B * a.H, a.r, 64);
+  const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
+  return launch_blocks(window_bwd_f32_small_kernel<D>, n_kv + q.grid.blocks, 64 * kWaves, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
 }
 
 template <int D>
@@ -410,6 +486,14 @@ int launch_bwd_t(const KArgs& a, bool dq_last, hipStream_t st) {
 
 int launch_fwd_f32_small(const KArgs& a, hipStream_t st) {
   return a.D == 64 ? launch_fwd_t<64>(a, st) : launch_fwd_t<128>(a, st);
+}
+
+int launch_window_fwd_f32_small(const KArgs& a, Win win, hipStream_t st) {
+  return a.D == 64 ? launch_window_fwd_t<64>(a, win, st) : launch_window_fwd_t<128>(a, win, st);
+}
+
+int launch_window_bwd_f32_small(const KArgs& a, Win win, hipStream_t st) {
+  return a.D == 64 ? launch_window_bwd_t<64>(a, win, st) : launch_window_bwd_t<128>(a, win, st);
 }
 
 int launch_bwd_f32_small(const KArgs& a, bool dq_last, hipStream_t st) {

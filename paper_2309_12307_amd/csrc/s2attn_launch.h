@@ -38,13 +38,18 @@ int launch_delta_bf16(const KArgs& a, hipStream_t st);
 int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st);
 
 // Window attention: forward; dK/dV and dQ (bf16: delta must be ready), dk, dv of cut key tiles left as partials; their sum
-int launch_window_fwd_f32(const KArgs& a, const Win& win, hipStream_t st);
-int launch_window_bwd_f32(const KArgs& a, const Win& win, hipStream_t st);
-int launch_window_fwd_bf16(const KArgs& a, const Win& win, hipStream_t st);
+int launch_window_fwd_f32(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_f32(const KArgs& a, Win win, hipStream_t st);
+int launch_window_fwd_bf16(const KArgs& a, Win win, hipStream_t st);
 int launch_window_bwd_bf16(const KArgs& a, Win win, hipStream_t st);
-int launch_window_fwd_d64(const KArgs& a, const Win& win, hipStream_t st);
+int launch_window_fwd_d64(const KArgs& a, Win win, hipStream_t st);
 int launch_window_bwd_d64(const KArgs& a, Win win, hipStream_t st);
-int launch_sink_combine(const KArgs& a, const Win& win, int dtype, hipStream_t st);
+// the same for few rows (bf16: D = 128), delta included
+int launch_window_fwd_f32_small(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_f32_small(const KArgs& a, Win win, hipStream_t st);
+int launch_window_fwd_small(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_small(const KArgs& a, Win win, hipStream_t st);
+int launch_sink_combine(const KArgs& a, const Win& win, int dtype, bool small, hipStream_t st);   // small: after those
 
 // current device is gfx950: an S2ATTN_* code
 int check_device();
@@ -111,6 +116,35 @@ inline Grid grid_of(int T, int n_seq, int share, int slots, bool crowded = false
   const int each = (n_seq / bundle + 7) / 8 * bundle;   // sequences of one XCD
   const int il = walk_of(T, each, bundle, slots, crowded);
   return Grid{8 * T * pad_to(each, il), Deal{n_seq, bundle, il, div_by(bundle), div_by(il), div_by(T * il)}};
+}
+
+// The same for `n_seq` sequences of `tiles` row tiles under a window, where only neighbouring tiles read the same keys: sequences are
+// cut into the fewest stretches (a power of two, of four tiles or more) that deal every XCD the same number.  Forward, us,
+// fp32, D = 64, two heads, N = 8192, window 512 on two XCDs and on eight: 97 and 36; backward 306 and 128.
+struct WindowGrid {
+  int T, cut;
+  Grid grid;
+};
+inline WindowGrid window_grid(int tiles, int n_seq, int share, int slots) {
+  int cut = 1;
+  while (n_seq * cut % 8 != 0 && tiles >= 8 * cut) cut *= 2;
+  const int T = (tiles + cut - 1) / cut;
+  return WindowGrid{T, cut, grid_of(T, n_seq * cut, cut == 1 ? share : 1, slots)};
+}
+inline WindowGrid window_grid_q(Win& win, int tiles, int n_seq, int share, int slots) {
+  const WindowGrid g = window_grid(tiles, n_seq, share, slots);
+  win.tiles = tiles;
+  win.cut_q = g.cut;
+  win.by_cut_q = div_by(g.cut);
+  return g;
+}
+inline WindowGrid window_grid_kv(Win& win, int tiles, int n_seq, int slots) {
+  const WindowGrid g = window_grid(tiles, n_seq, 1, slots);
+  win.tiles = tiles;
+  win.cut_kv = g.cut;
+  win.by_cut_kv = div_by(g.cut);
+  win.n_main = g.grid.blocks;
+  return g;
 }
 
 // Launches `blocks` blocks of `threads` threads as kernel(args..., first_block).  A launch counts the work items of

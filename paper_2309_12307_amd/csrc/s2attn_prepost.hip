@@ -111,34 +111,38 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* partial, void
 // dk, dv of the keys whose queries were cut into segments: the sum of all parts and segments, in order.  KT, QT: keys of a
 // key tile and queries of a query tile of the kernel that left them.
 template <bool BF16, int KT, int QT>
-__global__ void __launch_bounds__(256) sink_combine_kernel(KArgs a, Win win, Div by_row, Div by_keys) {
-  const int rows = win.sink_tiles * KT, i4 = block_id() * 256 + thread_id();
-  const int d4 = a.D / 4;
+__global__ void __launch_bounds__(256) sink_combine_kernel(KArgs a, Win win, Div by_row, Div by_keys, Div by_Hkv, int half) {
+  const int rows = win.sink_tiles * KT, d4 = a.D / 4;
+  const int which = block_id() >= half, i4 = (block_id() - (which ? half : 0)) * 256 + thread_id();   // dk, then dv
   const int row = quot(i4, by_row), d = (i4 - row * d4) * 4;
   const int bc = quot(row, by_keys), key = row - bc * rows;
-  const int b = bc / a.Hkv, c = bc - b * a.Hkv;
+  const int b = quot(bc, by_Hkv), c = bc - b * a.Hkv;
   if (b >= a.B || key >= a.N) return;
-  const int jt = key / KT;
-  int segments = 1;
-  while (segments <= win.n_seg && query_tiles<KT, QT>(win, a.N, jt, segments).lo < query_tiles<KT, QT>(win, a.N, jt, segments).hi) ++segments;
+  // segments that exist: those that begin before the last query tile of the key tile
+  const QueryTiles main = query_tiles<KT, QT>(win, a.N, key / KT, 0);
+  const int all = (a.N - key / KT * KT + QT - 1) / QT;
+  const int segments = 1 + min(win.n_seg, (all - main.hi + win.seg_tiles - 1) / win.seg_tiles);
+  const size_t step = (size_t)a.B * a.Hkv * rows * a.D;   // from one segment to the next
+  const float* src = far_row(win, a, which, 0, 0, b, c, key, KT) + d;
+  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int part = 0; part < a.parts; ++part, src += (1 + win.n_seg) * step)
+    for (int s0 = 0; s0 < segments; s0 += 4) {
+      float4 x[4];
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int part = 0; part < a.parts; ++part)
-      for (int segment = 0; segment < segments; ++segment) {
-        const float4 x = *reinterpret_cast<const float4*>(far_row(win, a, which, part, segment, b, c, key, KT) + d);
-        r.x += x.x; r.y += x.y; r.z += x.z; r.w += x.w;
-      }
-    const size_t o = row_off(which == 0 ? a.sdk : a.sdv, b, key, c) + d;
-    void* out = which == 0 ? a.dk : a.dv;
-    if (BF16) {
-      uint2 pk;
-      pk.x = f32_to_bf16_bits(r.x) | (f32_to_bf16_bits(r.y) << 16);
-      pk.y = f32_to_bf16_bits(r.z) | (f32_to_bf16_bits(r.w) << 16);
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + o) = pk;
-    } else {
-      *reinterpret_cast<float4*>(static_cast<float*>(out) + o) = r;
+      for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const float4*>(src + min(s0 + u, segments - 1) * step);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (s0 + u < segments) { r.x += x[u].x; r.y += x[u].y; r.z += x[u].z; r.w += x[u].w; }
     }
+  const size_t o = row_off(which == 0 ? a.sdk : a.sdv, b, key, c) + d;
+  void* out = which == 0 ? a.dk : a.dv;
+  if (BF16) {
+    uint2 pk;
+    pk.x = f32_to_bf16_bits(r.x) | (f32_to_bf16_bits(r.y) << 16);
+    pk.y = f32_to_bf16_bits(r.z) | (f32_to_bf16_bits(r.w) << 16);
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + o) = pk;
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + o) = r;
   }
 }
 
@@ -158,14 +162,18 @@ int launch_delta_bf16(const KArgs& a, hipStream_t st) {
   return a.D == 64 ? launch_delta_t<64, 2>(a, st) : launch_delta_t<128, 2>(a, st);
 }
 
-int launch_sink_combine(const KArgs& a, const Win& win, int dtype, hipStream_t st) {
-  const int rows = win.sink_tiles * (dtype == S2ATTN_BF16 ? 128 : 64), d4 = a.D / 4;
-  const dim3 grid((unsigned)(((long long)a.B * a.Hkv * rows * d4 + 255) / 256));
-  if (dtype == S2ATTN_BF16)
-    hipLaunchKernelGGL((sink_combine_kernel<true, 128, 64>), grid, dim3(256), 0, st, a, win, div_by(d4), div_by(rows));
-  else
-    hipLaunchKernelGGL((sink_combine_kernel<false, 64, 32>), grid, dim3(256), 0, st, a, win, div_by(d4), div_by(rows));
+template <bool BF16, int KT, int QT>
+static int launch_sink_combine_t(const KArgs& a, const Win& win, hipStream_t st) {
+  const int rows = win.sink_tiles * KT, d4 = a.D / 4;
+  const int half = (int)(((long long)a.B * a.Hkv * rows * d4 + 255) / 256);
+  hipLaunchKernelGGL((sink_combine_kernel<BF16, KT, QT>), dim3(2 * half), dim3(256), 0, st, a, win, div_by(d4), div_by(rows),
+                     div_by(a.Hkv), half);
   return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+int launch_sink_combine(const KArgs& a, const Win& win, int dtype, bool small, hipStream_t st) {
+  if (dtype == S2ATTN_BF16) return small ? launch_sink_combine_t<true, 32, 32>(a, win, st) : launch_sink_combine_t<true, 128, 64>(a, win, st);
+  return small ? launch_sink_combine_t<false, 16, 16>(a, win, st) : launch_sink_combine_t<false, 64, 32>(a, win, st);
 }
 
 int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st) {
