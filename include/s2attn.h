@@ -212,10 +212,11 @@ S2ATTN_API int s2attn_bwd_ex_marked(const s2attn_params* p, void* stream, void* 
  * there are no groups and no head shifts, N may be any positive number and H may be odd.
  * window >= 1; window >= N is plain causal attention.  sinks >= 0.  S2ATTN_ERR_WINDOW otherwise.
  * A batch padded on the right needs nothing: no token sees a later one, and padding rows with dout = 0 leave
- * the gradients of the others alone (k, v, dout of padding rows have to be finite). */
+ * the gradients of the others alone.  All of q, k, v, dout has to be finite, what no row sees included: a hidden product is
+ * multiplied by zero, not left out. */
 S2ATTN_API int s2attn_check_window_args(const s2attn_params* p, int window, int sinks, int backward);
 /* Bytes of device workspace the backward wants; 0 if the shape fields are invalid.  It runs with less, down to the row terms
- * (bf16) and the partial dk, dv of the sinks. */
+ * and the partial dk, dv of the sinks. */
 S2ATTN_API size_t s2attn_window_workspace_bytes(const s2attn_params* p, int window, int sinks);
 S2ATTN_API int s2attn_window_fwd(const s2attn_params* p, int window, int sinks, void* stream);
 S2ATTN_API int s2attn_window_bwd(const s2attn_params* p, int window, int sinks, void* stream);

@@ -597,13 +597,14 @@ int s2attn_window_bwd(const s2attn_params* p, int window, int sinks, void* strea
   if (a.parts > 1) a.dkv_partial = reinterpret_cast<float*>(ws + x.rows);
   x.win.partial = reinterpret_cast<float*>(ws + x.rows + x.partial);
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool dq_last = dq_reuses_input(p);
   if (p->dtype == S2ATTN_F32) {
-    rc = x.small_bwd ? s2::launch_window_bwd_f32_small(a, x.win, st) : s2::launch_window_bwd_f32(a, x.win, st);
+    rc = x.small_bwd ? s2::launch_window_bwd_f32_small(a, x.win, dq_last, st) : s2::launch_window_bwd_f32(a, x.win, dq_last, st);
   } else if (x.small_bwd) {
-    rc = s2::launch_window_bwd_small(a, x.win, st);
+    rc = s2::launch_window_bwd_small(a, x.win, dq_last, st);
   } else {
     rc = s2::launch_delta_bf16(a, st);
-    if (rc == 0) rc = s2::launch_window_bwd_bf16(a, x.win, st);
+    if (rc == 0) rc = s2::launch_window_bwd_bf16(a, x.win, dq_last, st);
   }
   // (the parts' sum leaves cut key tiles to the sum of their segments, which comes after it)
   if (rc == 0 && a.parts > 1) rc = s2::launch_combine_partials(a, p->dtype, st);

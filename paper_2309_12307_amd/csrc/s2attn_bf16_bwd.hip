@@ -472,8 +472,8 @@ int launch_bwd_dkdv_bf16(const KArgs& a, hipStream_t st) {
   return launch_blocks(bwd_dkdv_split_kernel<false, false>, g.blocks, 512, st, a, T, g.deal);
 }
 
-int launch_window_bwd_bf16(const KArgs& a, Win win, hipStream_t st) {
-  if (a.D == 64) return launch_window_bwd_d64(a, win, st);
+int launch_window_bwd_bf16(const KArgs& a, Win win, bool dq_last, hipStream_t st) {   // D = 128: dQ is always the last
+  if (a.D == 64) return launch_window_bwd_d64(a, win, dq_last, st);
   const int tiles = ragged_tiles(a, 128), n_seq = a.B * a.Hkv * a.parts;
   const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 32);
   const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);

@@ -656,11 +656,13 @@ int launch_window_fwd_d64(const KArgs& a, Win win, hipStream_t st) {
   return launch_blocks(window_fwd_d64_kernel, g.grid.blocks, 256, st, a, g.T, g.grid.deal, win);
 }
 
-int launch_window_bwd_d64(const KArgs& a, Win win, hipStream_t st) {
+int launch_window_bwd_d64(const KArgs& a, Win win, bool dq_last, hipStream_t st) {
   const int tiles = ragged_tiles(a, kOwn), n_seq = a.B * a.Hkv * a.parts;
   const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 64), q = window_grid_q(win, tiles, a.B * a.H, a.r, 64);
   const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
-  return launch_blocks(window_bwd_d64_kernel, n_kv + q.grid.blocks, 256, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
+  const int rc = launch_blocks(window_bwd_d64_kernel, dq_last ? n_kv : n_kv + q.grid.blocks, 256, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
+  if (rc != 0 || !dq_last) return rc;
+  return launch_blocks(window_bwd_d64_kernel, q.grid.blocks, 256, st, a, 0, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
 }
 
 int launch_bwd_dkdv_d64(const KArgs& a, hipStream_t st) {

@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(256) cache_kernel(PArgs a, int tokens, Div by_
     if (b[0] >= 0) {
       const SeqRows sr = seq_rows(a, b[0]);
       mine[0] = t0 >= sr.s0 && t0 < sr.s0 + sr.n;           // else: a row of no sequence
-      if (mine[0]) at[0] = cache_row(a, b[0], sr.kv - sr.n + t0 - sr.s0, sr.keys);
+      if (mine[0]) at[0] = cache_row(a, b[0], sr.kv - sr.n + (t0 - sr.s0), sr.keys);
     }
 #pragma unroll
     for (int s = 1; s < kSteps; ++s) { at[s] = at[0]; mine[s] = mine[0]; }
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(256) cache_kernel(PArgs a, int tokens, Div by_
       if (b[s] >= 0) {
         const SeqRows sr = seq_rows(a, b[s]);
         mine[s] = t[s] >= sr.s0 && t[s] < sr.s0 + sr.n;
-        if (mine[s]) at[s] = cache_row(a, b[s], sr.kv - sr.n + t[s] - sr.s0, sr.keys);
+        if (mine[s]) at[s] = cache_row(a, b[s], sr.kv - sr.n + (t[s] - sr.s0), sr.keys);
       }
     }
   }

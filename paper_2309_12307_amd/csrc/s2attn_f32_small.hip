@@ -458,11 +458,13 @@ int launch_window_fwd_t(const KArgs& a, Win win, hipStream_t st) {
 }
 
 template <int D>
-int launch_window_bwd_t(const KArgs& a, Win win, hipStream_t st) {
+int launch_window_bwd_t(const KArgs& a, Win win, bool dq_last, hipStream_t st) {
   const int tiles = ragged_tiles(a, kRows), n_seq = a.B * a.Hkv * a.parts;
   const WindowGrid kv = window_grid_kv(win, tiles, n_seq, 64), q = window_grid_q(win, tiles, a.B * a.H, a.r, 64);
   const int n_kv = pad_to(kv.grid.blocks + n_seq * win.sink_tiles * win.n_seg, 8);   // an XCD is the block number mod 8
-  return launch_blocks(window_bwd_f32_small_kernel<D>, n_kv + q.grid.blocks, 64 * kWaves, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
+  const int rc = launch_blocks(window_bwd_f32_small_kernel<D>, dq_last ? n_kv : n_kv + q.grid.blocks, 64 * kWaves, st, a, n_kv, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
+  if (rc != 0 || !dq_last) return rc;
+  return launch_blocks(window_bwd_f32_small_kernel<D>, q.grid.blocks, 64 * kWaves, st, a, 0, kv.T, kv.grid.deal, q.T, q.grid.deal, win);
 }
 
 template <int D>
@@ -492,8 +494,8 @@ int launch_window_fwd_f32_small(const KArgs& a, Win win, hipStream_t st) {
   return a.D == 64 ? launch_window_fwd_t<64>(a, win, st) : launch_window_fwd_t<128>(a, win, st);
 }
 
-int launch_window_bwd_f32_small(const KArgs& a, Win win, hipStream_t st) {
-  return a.D == 64 ? launch_window_bwd_t<64>(a, win, st) : launch_window_bwd_t<128>(a, win, st);
+int launch_window_bwd_f32_small(const KArgs& a, Win win, bool dq_last, hipStream_t st) {
+  return a.D == 64 ? launch_window_bwd_t<64>(a, win, dq_last, st) : launch_window_bwd_t<128>(a, win, dq_last, st);
 }
 
 int launch_bwd_f32_small(const KArgs& a, bool dq_last, hipStream_t st) {

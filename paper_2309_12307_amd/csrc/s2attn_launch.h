@@ -39,16 +39,16 @@ int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st);
 
 // Window attention: forward; dK/dV and dQ (bf16: delta must be ready), dk, dv of cut key tiles left as partials; their sum
 int launch_window_fwd_f32(const KArgs& a, Win win, hipStream_t st);
-int launch_window_bwd_f32(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_f32(const KArgs& a, Win win, bool dq_last, hipStream_t st);
 int launch_window_fwd_bf16(const KArgs& a, Win win, hipStream_t st);
-int launch_window_bwd_bf16(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_bf16(const KArgs& a, Win win, bool dq_last, hipStream_t st);
 int launch_window_fwd_d64(const KArgs& a, Win win, hipStream_t st);
-int launch_window_bwd_d64(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_d64(const KArgs& a, Win win, bool dq_last, hipStream_t st);
 // the same for few rows (bf16: D = 128), delta included
 int launch_window_fwd_f32_small(const KArgs& a, Win win, hipStream_t st);
-int launch_window_bwd_f32_small(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_f32_small(const KArgs& a, Win win, bool dq_last, hipStream_t st);
 int launch_window_fwd_small(const KArgs& a, Win win, hipStream_t st);
-int launch_window_bwd_small(const KArgs& a, Win win, hipStream_t st);
+int launch_window_bwd_small(const KArgs& a, Win win, bool dq_last, hipStream_t st);
 int launch_sink_combine(const KArgs& a, const Win& win, int dtype, bool small, hipStream_t st);   // small: after those
 
 // current device is gfx950: an S2ATTN_* code

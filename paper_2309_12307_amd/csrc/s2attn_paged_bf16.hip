@@ -104,7 +104,7 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
   if (b < 0) return;
   const SeqRows sr = seq_rows(a, b);
   const int i0 = uni((tile - first_tile<kRowsLog2>(a, b)) * kRows), n_rows = uni(sr.n * a.r);
-  if (i0 >= n_rows || n_rows <= a.few_rows) return;
+  if (i0 < 0 || i0 >= n_rows || n_rows <= a.few_rows) return;   // (less than 0: row_start falls somewhere)
   const int p_first = uni(sr.kv - sr.n);                        // position of the sequence's first row
   const int p_lo = uni(p_first + quot(i0, a.by_r));
   const int p_hi = uni(p_first + quot(min(i0 + kRows, n_rows) - 1, a.by_r));
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
   if (b < 0) return;
   const SeqRows sr = seq_rows(a, b);
   const int i0 = uni((tile - first_tile<kLog2>(a, b)) * kRows8), n_rows = uni(sr.n * a.r);
-  if (i0 >= n_rows || n_rows <= a.few_rows) return;
+  if (i0 < 0 || i0 >= n_rows || n_rows <= a.few_rows) return;   // (less than 0: row_start falls somewhere)
   const int p_first = uni(sr.kv - sr.n);
   const int p_lo = uni(p_first + quot(i0, a.by_r));
   const int p_hi = uni(p_first + quot(min(i0 + kRows8, n_rows) - 1, a.by_r));

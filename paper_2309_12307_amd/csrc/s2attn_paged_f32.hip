@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   if (b < 0) return;
   const SeqRows sr = seq_rows(a, b);
   const int i0 = uni((tile - first_tile<kRowsLog2>(a, b)) * kWgRows), n_rows = uni(sr.n * a.r);
-  if (i0 >= n_rows) return;
+  if (i0 < 0 || i0 >= n_rows) return;   // (less than 0: row_start falls somewhere)
   const int p_first = uni(sr.kv - sr.n);
   const int p_lo = uni(p_first + quot(i0, a.by_r));
   const int p_hi = uni(p_first + quot(min(i0 + kWgRows, n_rows) - 1, a.by_r));
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, int nq, int he
   const int b = find_seq<-1>(a, t, tid & 63);
   if (b < 0) return;
   const SeqRows sr = seq_rows(a, b);
-  if (t >= sr.s0 + sr.n) return;
+  if (t < sr.s0 || t >= sr.s0 + sr.n) return;
   const int n_rows = sr.n * a.r, p_first = sr.kv - sr.n;
   const bool few = n_rows <= a.few_rows;
   const int tile = few ? 16 * nq : a.chunk_rows;
