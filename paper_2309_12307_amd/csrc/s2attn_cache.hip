@@ -176,44 +176,28 @@ __global__ void __launch_bounds__(256) cache_kernel(PArgs a, int tokens, Div by_
     }
   }
 
-  // the places of the tokens
-  int b[kSteps];
-  if (tokens == 1) {
-    const int one = find_seq<-1>(a, t0, lane);
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) b[s] = one;
-  } else {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) b[s] = -1;
-    for (int u = 0; u < tokens && t0 + u < a.T; ++u) {
-      const int one = find_seq<-1>(a, t0 + u, lane);
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) b[s] = t[s] == t0 + u ? one : b[s];
-    }
-  }
-  CacheRow at[kSteps];
+  // the places of the tokens: their sequences' positions, and whether they are rows of one
+  int b[kSteps], pos[kSteps], keys[kSteps];
   bool mine[kSteps];
+  CacheRow at[kSteps];
   if (tokens == 1) {
-    at[0] = CacheRow{-1, 0};
-    mine[0] = false;
-    if (b[0] >= 0) {
-      const SeqRows sr = seq_rows(a, b[0]);
-      mine[0] = t0 >= sr.s0 && t0 < sr.s0 + sr.n;           // else: a row of no sequence
-      if (mine[0]) at[0] = cache_row(a, b[0], sr.kv - sr.n + (t0 - sr.s0), sr.keys);
-    }
+    const SeqRows sr = find_rows<-1>(a, t0, lane);
+    const bool in = sr.b >= 0 && t0 >= sr.s0 && t0 < sr.s0 + sr.n;
+    const CacheRow one = in ? cache_row(a, sr.b, sr.kv - sr.n + (t0 - sr.s0), sr.keys) : CacheRow{-1, 0};
 #pragma unroll
-    for (int s = 1; s < kSteps; ++s) { at[s] = at[0]; mine[s] = mine[0]; }
+    for (int s = 0; s < kSteps; ++s) { at[s] = one; mine[s] = in; }
   } else {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      at[s] = CacheRow{-1, 0};
-      mine[s] = false;
-      if (b[s] >= 0) {
-        const SeqRows sr = seq_rows(a, b[s]);
-        mine[s] = t[s] >= sr.s0 && t[s] < sr.s0 + sr.n;
-        if (mine[s]) at[s] = cache_row(a, b[s], sr.kv - sr.n + (t[s] - sr.s0), sr.keys);
-      }
+    for (int s = 0; s < kSteps; ++s) { b[s] = 0; pos[s] = -1; keys[s] = 0; mine[s] = false; }
+    for (int u = 0; u < tokens && t0 + u < a.T; ++u) {
+      const SeqRows sr = find_rows<-1>(a, t0 + u, lane);
+      const bool in = sr.b >= 0 && t0 + u >= sr.s0 && t0 + u < sr.s0 + sr.n;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+        if (in && t[s] == t0 + u) { b[s] = sr.b; pos[s] = sr.kv - sr.n + (t0 + u - sr.s0); keys[s] = sr.keys; mine[s] = true; }
     }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) at[s] = cache_row(a, b[s], pos[s], keys[s]);
   }
   u32x4 y[kSteps];
   float scale[kSteps];

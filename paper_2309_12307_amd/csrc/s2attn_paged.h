@@ -54,25 +54,37 @@ __device__ __forceinline__ SeqRows seq_rows(const PArgs& a, int b) {
   return s;
 }
 
-// The number of sequences whose first unit is at or before `id`, less one: units are packed rows (SHIFT < 0) or row
-// tiles of 2^SHIFT (token, query head of the kv head) pairs, of which sequence b owns those from
+// The last sequence whose first unit is at or before `id` (b = -1: none): units are packed rows (SHIFT < 0) or row
+// tiles of 2^SHIFT (token, query head of the kv head) pairs, of which a sequence owns those from
 // (row_start[b] * r >> SHIFT) + b on: at least as many as it needs, and no running sum is needed to place them.
-// The whole wave calls it: 64 sequences a step, one answer.
+// The whole wave calls it and has one answer: up to 64 sequences are looked at together, everything about them read at once;
+// more are narrowed down by looking at every 64th part first.  Where row_start falls, the answer is some sequence.
 template <int SHIFT>
-__device__ __forceinline__ int first_tile(const PArgs& a, int b) { return (int)((unsigned)(start_of(a, b) * a.r) >> SHIFT) + b; }
+__device__ __forceinline__ int first_tile(const PArgs& a, int s0, int b) { return (int)((unsigned)(s0 * a.r) >> SHIFT) + b; }
 template <int SHIFT>
-__device__ __forceinline__ int find_seq(const PArgs& a, int id, int lane) {
-  int n = 0;
-  for (int i0 = 0; i0 < a.B; i0 += 64) {
-    const int i = i0 + lane;
-    bool before = false;
-    if (i < a.B) {
-      if constexpr (SHIFT < 0) before = start_of(a, i) <= id;
-      else before = first_tile<SHIFT>(a, i) <= id;
-    }
-    n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+__device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane) {
+  auto before = [&](int start, int i) __attribute__((always_inline)) {
+    const int s0 = min(max(start, 0), a.T);
+    if constexpr (SHIFT < 0) return s0 <= id;
+    else return first_tile<SHIFT>(a, s0, i) <= id;
+  };
+  int lo = 0, hi = a.B;
+  while (hi - lo > 64) {
+    const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
+    const int m = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && before(a.row_start[min(i, hi - 1)], i)));
+    lo += max(wave_uniform(m) - 1, 0) * step;
+    hi = min(hi, lo + step);
   }
-  return wave_uniform(n - 1);
+  const int i = min(lo + lane, hi - 1);
+  const int start = a.row_start[i], end = a.row_start[i + 1], kv = a.kv_len[i];
+  const int l = wave_uniform(__builtin_popcountll(__builtin_amdgcn_ballot_w64(lo + lane < hi && before(start, i)))) - 1;
+  SeqRows s;
+  s.b = l < 0 ? -1 : lo + l;
+  s.s0 = min(max(__builtin_amdgcn_readlane(start, max(l, 0)), 0), a.T);
+  s.n = max(min(max(__builtin_amdgcn_readlane(end, max(l, 0)), 0), a.T) - s.s0, 0);
+  s.kv = max(__builtin_amdgcn_readlane(kv, max(l, 0)), 0);
+  s.keys = min(s.kv, a.max_keys);
+  return s;
 }
 
 // Block -> (row tile, kv head, split).  Blocks of one (kv head, split) read the same keys: whole such groups go to an XCD

@@ -100,10 +100,10 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
   const int g32 = lane >> 5, l32 = lane & 31;
   int tile, c, split;
   if (!tile_of_block(a, a.chunk, block, tile, c, split)) return;
-  const int b = find_seq<kRowsLog2>(a, tile, lane);
+  const SeqRows sr = find_rows<kRowsLog2>(a, tile, lane);
+  const int b = sr.b;
   if (b < 0) return;
-  const SeqRows sr = seq_rows(a, b);
-  const int i0 = uni((tile - first_tile<kRowsLog2>(a, b)) * kRows), n_rows = uni(sr.n * a.r);
+  const int i0 = uni((tile - first_tile<kRowsLog2>(a, sr.s0, b)) * kRows), n_rows = uni(sr.n * a.r);
   if (i0 < 0 || i0 >= n_rows || n_rows <= a.few_rows) return;   // (less than 0: row_start falls somewhere)
   const int p_first = uni(sr.kv - sr.n);                        // position of the sequence's first row
   const int p_lo = uni(p_first + quot(i0, a.by_r));
@@ -346,10 +346,10 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
   const int g32 = lane >> 5, l32 = lane & 31;
   int tile, c, split;
   if (!tile_of_block(a, a.chunk, first_block + block_id(), tile, c, split)) return;
-  const int b = find_seq<kLog2>(a, tile, lane);
+  const SeqRows sr = find_rows<kLog2>(a, tile, lane);
+  const int b = sr.b;
   if (b < 0) return;
-  const SeqRows sr = seq_rows(a, b);
-  const int i0 = uni((tile - first_tile<kLog2>(a, b)) * kRows8), n_rows = uni(sr.n * a.r);
+  const int i0 = uni((tile - first_tile<kLog2>(a, sr.s0, b)) * kRows8), n_rows = uni(sr.n * a.r);
   if (i0 < 0 || i0 >= n_rows || n_rows <= a.few_rows) return;   // (less than 0: row_start falls somewhere)
   const int p_first = uni(sr.kv - sr.n);
   const int p_lo = uni(p_first + quot(i0, a.by_r));

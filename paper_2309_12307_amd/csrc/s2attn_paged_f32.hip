@@ -24,10 +24,10 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   const int c16 = lane & 15, q4 = lane >> 4;
   int tile, c, split;
   if (!tile_of_block(a, a.chunk, first_block + block_id(), tile, c, split)) return;
-  const int b = find_seq<kRowsLog2>(a, tile, lane);
+  const SeqRows sr = find_rows<kRowsLog2>(a, tile, lane);
+  const int b = sr.b;
   if (b < 0) return;
-  const SeqRows sr = seq_rows(a, b);
-  const int i0 = uni((tile - first_tile<kRowsLog2>(a, b)) * kWgRows), n_rows = uni(sr.n * a.r);
+  const int i0 = uni((tile - first_tile<kRowsLog2>(a, sr.s0, b)) * kWgRows), n_rows = uni(sr.n * a.r);
   if (i0 < 0 || i0 >= n_rows) return;   // (less than 0: row_start falls somewhere)
   const int p_first = uni(sr.kv - sr.n);
   const int p_lo = uni(p_first + quot(i0, a.by_r));
@@ -410,19 +410,18 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
 
 // o = sum of the pieces' outputs by their share exp2(lse_s - lse) of the row.  D / 4 lanes hold a piece's output; G groups of so
 // many lanes take the pieces of one row, four at a time (each group with a running maximum of its own), the other groups of a
-// workgroup other heads of the same token, `heads` of them to a workgroup.
+// workgroup other heads of the same token, `heads` of them to a workgroup.  Bound by latency: six workgroups to a CU hide it
+// better than the four that the compiler would have left room for (13.4 and 11.2 us for the case below).
 template <int D, int TK, int FEW_TK, bool BF16>
-__global__ void __launch_bounds__(256) paged_join_kernel(PArgs a, int nq, int heads, int head_blocks, Div by_head_blocks, int first_block) {
+__global__ void __launch_bounds__(256, 6) paged_join_kernel(PArgs a, int nq, int heads, int head_blocks, Div by_head_blocks, int first_block) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
   __shared__ float4 acc_s[kGroups][kLanes];
   __shared__ float m_s[kGroups], l_s[kGroups];
   const int tid = thread_id(), H = a.Hkv * a.r;
   const int block = first_block + block_id(), t = quot(block, by_head_blocks), h0 = (block - t * head_blocks) * heads;
   if (t >= a.T) return;
-  const int b = find_seq<-1>(a, t, tid & 63);
-  if (b < 0) return;
-  const SeqRows sr = seq_rows(a, b);
-  if (t < sr.s0 || t >= sr.s0 + sr.n) return;
+  const SeqRows sr = find_rows<-1>(a, t, tid & 63);
+  if (sr.b < 0 || t < sr.s0 || t >= sr.s0 + sr.n) return;
   const int n_rows = sr.n * a.r, p_first = sr.kv - sr.n;
   const bool few = n_rows <= a.few_rows;
   const int tile = few ? 16 * nq : a.chunk_rows;
@@ -499,9 +498,10 @@ template <int D, int TK, int FEW_TK, bool BF16>
 int join_t(const PArgs& a, int nq, hipStream_t st) {
   constexpr int kGroups = 1024 / D;
   const int H = a.Hkv * a.r, splits = a.few.splits > a.chunk.splits ? a.few.splits : a.chunk.splits;
-  // heads go together while 1024 workgroups are left
+  // heads go together while 2048 workgroups are left: 16 sequences of 1 to 600 rows, H = 32, D = 64, down to 512, 2048 and 4096
+  // 20, 10.0 and 11.2 us
   int heads = splits <= 4 ? kGroups : splits <= 8 ? kGroups / 2 : splits <= 16 ? kGroups / 4 : kGroups / 8;
-  while (2 * heads <= H && (long long)a.T * (H / (2 * heads)) >= 1024) heads *= 2;
+  while (2 * heads <= H && (long long)a.T * (H / (2 * heads)) >= 2048) heads *= 2;
   const int head_blocks = (H + heads - 1) / heads;
   return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16>, a.T * head_blocks, 256, st, a, nq, heads, head_blocks, div_by(head_blocks));
 }
