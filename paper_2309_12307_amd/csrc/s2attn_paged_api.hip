@@ -103,10 +103,15 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   const long long tile = x.chunk_rows, in_tile = std::min(tile, (rows + seqs - 1) / seqs);
   const long long tiles = std::max((rows + tile - 1) / tile, seqs);
   const long long min_keys = std::max<long long>(256, 8 * in_tile);
-  x.chunk_splits = x.chunk ? pieces(tiles * p->Hkv, in_tile <= 16 ? 2048 : x.chunk_rows == 256 ? 256 : 512, min_keys) : 1;
-  x.chunk_min = (int)(min_keys / tile_keys(p));
+  // As many pieces as the chip holds workgroups of the longest sequences' keys; shorter ones get pieces of about that length, not as
+  // many.  us, pieces of min_keys and of these: 16 sequences of 1 to 600 rows over up to 12 000 tokens, D = 64, in 512 workgroups
+  // 321, in 768 257 and 226; one row over 30 000 tokens, 16 sequences, e4m3 304 and 299; over 4000, 128 sequences 168 and 163;
+  // over 8192, 32 sequences 76.2 and 77.5.
+  const int resident = in_tile <= 16 ? 2048 : x.chunk_rows == 256 ? 256 : p->D == 64 ? 768 : 512;
+  x.chunk_splits = x.chunk ? pieces(tiles * p->Hkv, resident, min_keys) : 1;
+  x.chunk_min = (int)(std::max(min_keys, keys / x.chunk_splits * 3 / 4) / tile_keys(p));
   x.few_splits = x.few ? pieces(seqs * p->Hkv, 2048, 256) : 1;
-  x.few_min = 256 / (f32 ? 16 : 32);
+  x.few_min = (int)(std::max<long long>(256, keys / x.few_splits / 2) / (f32 ? 16 : 32));
   return x;
 }
 
