@@ -266,7 +266,8 @@ void window_small(const s2attn_params* p, bool& fwd, bool& bwd) {
 // segment then is a third of the other workgroups' chains, behind which it starts, but six query tiles or more (each leaves a
 // partial dk, dv), and longer where that would take over kMostSegments.  Backward, us, segments as long as the others and a
 // third: B = 2, N = 8192, H = 32, Hkv = 8, D = 128, window 1024 1195 and 1151, B = 1 662 and 603; H = 8, N = 4096, window 512
-// 90 and 82.  Less than six tiles: fp32, H = 8, N = 2048, D = 128, window 128 100 and 107.  With more sink tiles their
+// 90 and 82.  A 32nd of what a CU has to do in all is short enough: many sequences have few segments, and little workspace
+// for them.  Less than six tiles: fp32, H = 8, N = 2048, D = 128, window 128 100 and 107.  With more sink tiles their
 // workgroups take all queries, as in plain causal attention.
 // The query heads of a kv head go in parts until there are two workgroups to a CU, in parts of 1024 query rows (fp32: 256) or more.
 WindowPlan window_plan(const s2attn_params* p, int window, int sinks, size_t avail) {
@@ -281,7 +282,9 @@ WindowPlan window_plan(const s2attn_params* p, int window, int sinks, size_t ava
   const int main_tiles = std::min<long long>(all, (KT - 1LL + x.win.window + QT - 1) / QT);
   if (tiles > 0 && tiles <= kMostCutTiles && all > main_tiles) {
     x.win.sink_tiles = tiles;
+    const long long seqs = (long long)p->B * p->Hkv, work = seqs * ((p->N + KT - 1) / KT) * main_tiles + seqs * tiles * (all - main_tiles);
     x.win.seg_tiles = std::max(std::max(std::min(main_tiles, 6), (main_tiles + 2) / 3), (all - main_tiles + kMostSegments - 1) / kMostSegments);
+    x.win.seg_tiles = (int)std::min<long long>(std::max<long long>(x.win.seg_tiles, work / 256 / 32), all - main_tiles);
     x.win.n_seg = (all - main_tiles + x.win.seg_tiles - 1) / x.win.seg_tiles;
   }
   x.rows = 2 * delta_bytes(p->B, p->N, p->H);
