@@ -76,20 +76,22 @@ struct Plan {
 Plan plan(const s2attn_paged_params* p, bool by16) {
   Plan x{};
   const long long r = p->H / p->Hkv, rows = p->T * r, seqs = std::max(1, std::min(p->B, p->T));
-  // One token a sequence (as far as T and B tell): all go to `few`, which takes any number of rows, by turns.  Where some have
-  // more, those of up to 16 or 32 rows go there and the others to `chunk`.
-  // (fp32: all to one of the two.)
+  // One token a sequence (as far as T and B tell): all go to `few`, which takes any number of rows, by turns of 16 or 32.  Where
+  // some have more, those of up to 16 or 32 rows (fp32: 64, in turns) go there and the others to `chunk`.  us, all in `chunk` and all in
+  // `few`, 4000 keys, D = 128: fp32, one sequence of 16 rows 35.8 and 19.9, of 64 65.9 and 57.2, eight of 16 78 and 56; bf16, one of
+  // 16 15.2 and 14.6, of 48 20.7 and 24.4; one token of 32 sequences, H = 32, bf16 290 and 272, 16 over 30 000 keys, e4m3 558 and 300.
   const bool f32 = p->dtype == S2ATTN_F32;
+  const long long most_few = f32 ? 64 : 32;
   x.nq = 1;
-  if ((p->T <= p->B && r <= 32) || rows <= 32) {
+  if ((p->T <= p->B && r <= most_few) || rows <= most_few) {
     x.few = true;
     if (!f32 && (p->T <= p->B ? r : rows) > 16) x.nq = 2;
     x.few_rows = INT_MAX;
   } else {
     x.chunk = true;
-    x.few = !f32 && p->B > 1;
-    x.nq = rows <= 16 * seqs ? 1 : 2;
-    x.few_rows = x.few ? 16 * x.nq : 0;
+    x.few = p->B > 1;
+    if (!f32 && rows > 16 * seqs) x.nq = 2;
+    x.few_rows = !x.few ? 0 : f32 ? 64 : 16 * x.nq;
   }
   const long long most = (long long)p->table_cols * p->page_size;
   long long keys = p->max_kv > 0 ? std::min<long long>(p->max_kv, most) : most;
@@ -98,8 +100,11 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
     const long long n = std::min((keys + min_keys - 1) / min_keys, (target + blocks - 1) / blocks);
     return (int)std::max<long long>(1, std::min<long long>(n, 256));
   };
-  // Eight waves on 256 rows where the sequences are long and their tiles fill the chip.
-  x.chunk_rows = f32 ? 64 : by16 && p->D == 128 && rows / seqs >= 512 && rows / 256 * p->Hkv >= 256 ? 256 : 128;
+  // Eight waves on 256 rows where the sequences are long, if their tiles fill the chip or their pieces are long too.  us, four waves and
+  // eight, H = 32: one sequence of 4096 rows over 8000 keys 417 and 410, of 2048 over 32 000 (Hkv = 8) 1002 and 933; of 1024 over 8000 (two
+  // pieces) 151 and 146, of 512 (four) 90 and 93; H = 40, two of 700 over 3000 126 and 101; H = 8, eight of 512 over 4000 (two pieces) 90 and 116.
+  const long long wide = (rows + 255) / 256 * p->Hkv;
+  x.chunk_rows = f32 ? 64 : by16 && p->D == 128 && rows / seqs >= 512 && (wide >= 192 || keys * wide / 256 >= 4000) ? 256 : 128;
   const long long tile = x.chunk_rows, in_tile = std::min(tile, (rows + seqs - 1) / seqs);
   const long long tiles = std::max((rows + tile - 1) / tile, seqs);
   const long long min_keys = std::max<long long>(256, 8 * in_tile);

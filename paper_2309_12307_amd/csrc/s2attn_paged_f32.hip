@@ -15,20 +15,19 @@ constexpr int kRowsLog2 = 6;
 static_assert(kWgRows == 1 << kRowsLog2, "rows of a workgroup");
 
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_block) {
+__device__ __forceinline__ void chunk_f32_workgroup(const PArgs& a, int block, char* smem) {   // smem: [stage][K, V]
   using L = Lanes<D>;
   constexpr int kEsz = E4M3 ? 1 : 4;
-  __shared__ __attribute__((aligned(1024))) char smem[4 * L::kTileBytes];   // [stage][K, V]
 
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
   int tile, c, split;
-  if (!tile_of_block(a, a.chunk, first_block + block_id(), tile, c, split)) return;
+  if (!tile_of_block(a, a.chunk, block, tile, c, split)) return;
   const SeqRows sr = find_rows<kRowsLog2>(a, tile, lane);
   const int b = sr.b;
   if (b < 0) return;
   const int i0 = uni((tile - first_tile<kRowsLog2>(a, sr.s0, b)) * kWgRows), n_rows = uni(sr.n * a.r);
-  if (i0 < 0 || i0 >= n_rows) return;   // (less than 0: row_start falls somewhere)
+  if (i0 < 0 || i0 >= n_rows || n_rows <= a.few_rows) return;   // (less than 0: row_start falls somewhere)
   const int p_first = uni(sr.kv - sr.n);
   const int p_lo = uni(p_first + quot(i0, a.by_r));
   const int p_hi = uni(p_first + quot(min(i0 + kWgRows, n_rows) - 1, a.by_r));
@@ -207,7 +206,7 @@ __global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_bl
   if (q4 == 0 && a.lse) a.lse[(size_t)h * a.T + t] = lse2 * kLn2;
 }
 
-// ---- few rows: sixteen rows of a sequence, the waves on different tiles of 16 keys, K and V straight to registers, the next
+// ---- few rows: sixteen rows of a sequence at a time, the waves on different tiles of 16 keys, K and V straight to registers, the next
 // tile on its way while one is worked on (as in the bf16 kernel; operands as in s2attn_f32_small.hip).
 //   K  lane (c16, q4) has key c16: fp32 floats 16 i + 4 q4 .., e4m3 values 16 (q4 + 4 i) ..; Q agrees
 //   V  lane (c16, q4) has keys 4 q4 + v, values 64 j + 4 c16 ..
@@ -221,19 +220,17 @@ struct FewTile {
 };
 
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int first_block) {
+__device__ __forceinline__ void few_f32_workgroup(const PArgs& a, int block, float* blocks, float (*max_s)[16], float (*sum_s)[16]) {
   using T = FewTile<D, E4M3>;
   constexpr int TK = 16, kWaves = 4, kEsz = E4M3 ? 1 : 4, kStride = D + 4;
-  __shared__ __attribute__((aligned(16))) float blocks[kWaves * 16 * kStride];
-  __shared__ float max_s[kWaves][16], sum_s[kWaves][16];
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
-  const int block = first_block + block_id();
   const int y = quot(block, a.by_Hkv), c = block - y * a.Hkv;
   const int b = quot(y, a.few.by_splits), split = y - b * a.few.splits;
   if (b >= a.B) return;
   const SeqRows sr = seq_rows(a, b);
   const int n_rows = uni(sr.n * a.r), p_first = uni(sr.kv - sr.n);
+  if (n_rows > a.few_rows) return;
   const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz + 16 * q4;
   const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz + 4 * c16 * kEsz;
   const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
@@ -408,6 +405,36 @@ __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int firs
   }
 }
 
+template <int D>
+constexpr int kChunkBytes = 4 * Lanes<D>::kTileBytes;
+template <int D>
+constexpr int kFewBytes = 4 * 16 * (D + 4) * 4;
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(256, 2) paged_f32_kernel(PArgs a, int first_block) {
+  __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D>];
+  chunk_f32_workgroup<D, E4M3>(a, first_block + block_id(), smem);
+}
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int first_block) {
+  __shared__ __attribute__((aligned(16))) float blocks[kFewBytes<D> / 4];
+  __shared__ float max_s[4][16], sum_s[4][16];
+  few_f32_workgroup<D, E4M3>(a, first_block + block_id(), blocks, max_s, sum_s);
+}
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(256, 2) paged_both_f32_kernel(PArgs a, int first_block) {
+  static_assert(kFewBytes<D> <= kChunkBytes<D>, "one room for both");
+  __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D>];
+  __shared__ float max_s[4][16], sum_s[4][16];
+  const int block = first_block + block_id();
+  if (block < a.chunk_blocks)
+    chunk_f32_workgroup<D, E4M3>(a, block, smem);
+  else
+    few_f32_workgroup<D, E4M3>(a, block - a.chunk_blocks, reinterpret_cast<float*>(smem), max_s, sum_s);
+}
+
 // o = sum of the pieces' outputs by their share exp2(lse_s - lse) of the row.  D / 4 lanes hold a piece's output; G groups of so
 // many lanes take the pieces of one row, four at a time (each group with a running maximum of its own), the other groups of a
 // workgroup other heads of the same token, `heads` of them to a workgroup.  Bound by latency: six workgroups to a CU hide it
@@ -506,20 +533,19 @@ int join_t(const PArgs& a, int nq, hipStream_t st) {
   return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16>, a.T * head_blocks, 256, st, a, nq, heads, head_blocks, div_by(head_blocks));
 }
 
+template <int D, bool E4M3>
+int launch_pages(const PArgs& a, hipStream_t st) {
+  const int few = a.B * a.Hkv * a.few.splits;
+  if (a.chunk_blocks == 0) return launch_blocks(paged_few_f32_kernel<D, E4M3>, few, 256, st, a);
+  if (a.few_rows == 0) return launch_blocks(paged_f32_kernel<D, E4M3>, a.chunk_blocks, 256, st, a);
+  return launch_blocks(paged_both_f32_kernel<D, E4M3>, a.chunk_blocks + few, 256, st, a);
+}
+
 }  // namespace
 
 int launch_paged_f32(const PArgs& a, int D, bool e4m3, hipStream_t st) {
-  if (a.chunk_blocks == 0) {
-    const int few = a.B * a.Hkv * a.few.splits;
-    if (D == 64) return e4m3 ? launch_blocks(paged_few_f32_kernel<64, true>, few, 256, st, a)
-                             : launch_blocks(paged_few_f32_kernel<64, false>, few, 256, st, a);
-    return e4m3 ? launch_blocks(paged_few_f32_kernel<128, true>, few, 256, st, a)
-                : launch_blocks(paged_few_f32_kernel<128, false>, few, 256, st, a);
-  }
-  if (D == 64) return e4m3 ? launch_blocks(paged_f32_kernel<64, true>, a.chunk_blocks, 256, st, a)
-                           : launch_blocks(paged_f32_kernel<64, false>, a.chunk_blocks, 256, st, a);
-  return e4m3 ? launch_blocks(paged_f32_kernel<128, true>, a.chunk_blocks, 256, st, a)
-              : launch_blocks(paged_f32_kernel<128, false>, a.chunk_blocks, 256, st, a);
+  if (D == 64) return e4m3 ? launch_pages<64, true>(a, st) : launch_pages<64, false>(a, st);
+  return e4m3 ? launch_pages<128, true>(a, st) : launch_pages<128, false>(a, st);
 }
 
 int launch_paged_join(const PArgs& a, int D, bool bf16, int nq, hipStream_t st) {
