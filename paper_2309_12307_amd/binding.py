@@ -226,6 +226,8 @@ def make_params(q, k, v, o, lse, G, dout=None, dq=None, dk=None, dv=None, worksp
         B, N, H, Hkv, D = dims
     p = S2AttnParams()
     p.device = None if isinstance(q, int) else _device_of(q)
+    p.problem = None if isinstance(q, int) else _problem_of(
+        q, dict(k=k, v=v, dk=dk, dv=dv), dict(o=o, dout=dout, dq=dq), lse, (B, N, H, Hkv, D), strided)
     p.q, p.k, p.v, p.o, p.lse = _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse)
     p.dout, p.dq, p.dk, p.dv = _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv)
     p.workspace = _ptr(workspace)
@@ -242,6 +244,26 @@ def make_params(q, k, v, o, lse, G, dout=None, dq=None, dk=None, dv=None, worksp
                 raise ValueError("the head-dim axis must be contiguous")
             setattr(p, name + "_strides", (ctypes.c_longlong * 3)(t.stride(0), t.stride(1), t.stride(2)))
     return p
+
+
+def _problem_of(q, like_k, like_q, lse, dims, strided):
+    """What is wrong with a block's tensors (None: nothing): s2attn_window_fwd and s2attn_window_bwd refuse it."""
+    B, N, H, Hkv, D = dims
+    for shape, tensors in (((B, N, Hkv, D), like_k), ((B, N, H, D), dict(like_q, q=q))):
+        for name, t in tensors.items():
+            if t is None or isinstance(t, int):
+                continue
+            if t.shape != shape or t.dtype != q.dtype or t.device != q.device:
+                return f"{name} must be {shape} of q's type on q's device"
+            if name in ("o", "dout") or not strided:
+                if not t.is_contiguous():
+                    return f"{name} must be contiguous" + ("" if strided else " (or strided=True given)")
+            elif not any(t.stride()[:3]) and max(shape[:3]) > 1:   # all zero stands for contiguous
+                return f"{name} is one row, expanded"
+    if not (lse is None or isinstance(lse, int)):
+        if lse.shape != (B, H, N) or lse.element_size() != 4 or not lse.is_floating_point() or not lse.is_contiguous() or lse.device != q.device:
+            return f"lse must be a contiguous float32 {(B, H, N)} on q's device"
+    return None
 
 
 def check_args(p: S2AttnParams, backward: bool) -> int:
@@ -306,6 +328,12 @@ def _on_device(p):
         raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
+def _whole(p):
+    if getattr(p, "problem", None):
+        raise ValueError(p.problem)
+    _on_device(p)
+
+
 def check_window_args(p: S2AttnParams, window: int, sinks: int, backward: bool) -> int:
     return int(lib().s2attn_check_window_args(ctypes.byref(p), window, sinks, 1 if backward else 0))
 
@@ -318,7 +346,7 @@ def window_workspace_bytes(p: S2AttnParams, window: int, sinks: int = 0) -> int:
 def s2attn_window_fwd(p: S2AttnParams, window: int, sinks: int = 0, stream=None) -> None:
     """o, lse <- causal attention over the last `window` tokens and the first `sinks`; p from make_params, whose G and
     shift options are not read (pass G = 0)."""
-    _on_device(p)
+    _whole(p)
     code = (_lib or lib()).s2attn_window_fwd(ctypes.byref(p), window, sinks, _stream(stream))
     if code:
         _check(code)
@@ -326,7 +354,7 @@ def s2attn_window_fwd(p: S2AttnParams, window: int, sinks: int = 0, stream=None)
 
 def s2attn_window_bwd(p: S2AttnParams, window: int, sinks: int = 0, stream=None) -> None:
     """dq, dk, dv <- gradients of sum(o * dout) of s2attn_window_fwd."""
-    _on_device(p)
+    _whole(p)
     code = (_lib or lib()).s2attn_window_bwd(ctypes.byref(p), window, sinks, _stream(stream))
     if code:
         _check(code)
@@ -372,6 +400,8 @@ def make_paged_params(row_start, kv_len, page_table, k_cache, v_cache, k_exp=Non
     p.B = kv_len.shape[0]
     if row_start.shape[0] != p.B + 1 or page_table.shape[0] != p.B:
         raise ValueError("row_start must have B + 1 entries, page_table B rows")
+    if p.B > 1 and page_table.stride(0) == 0:    # zero stands for contiguous
+        raise ValueError("page_table is one row, expanded")
     p.pages, p.page_size, p.Hkv, p.D = k_cache.shape
     if v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
         raise ValueError("k_cache and v_cache must have one shape and type")

@@ -113,6 +113,7 @@ def test_binding_fills_the_block(cache):
 
 @pytest.mark.parametrize("change", [
     dict(row_start=torch.zeros(3, dtype=torch.int64)), dict(row_start=torch.zeros(2, dtype=torch.int32)), dict(kv_len=torch.zeros(2, 1, dtype=torch.int32)),
+    dict(page_table=torch.zeros(3, dtype=torch.int32).expand(2, 3)), dict(q=torch.zeros(1, 1, 64, dtype=torch.bfloat16).expand(5, 4, 64)),
     dict(page_table=torch.zeros(3, 3, dtype=torch.int32)), dict(page_table=torch.zeros(3, 2, dtype=torch.int32).t()),
     dict(v_cache=torch.zeros(6, 16, 2, 128, dtype=torch.bfloat16)), dict(v_cache=torch.zeros(6, 16, 2, 64)),
     dict(k_cache=torch.zeros(6, 16, 64, 2, dtype=torch.bfloat16).transpose(2, 3), v_cache=torch.zeros(6, 16, 64, 2, dtype=torch.bfloat16).transpose(2, 3)),

@@ -73,3 +73,22 @@ def test_reference_gradients_are_autograds(window, sinks):
     for name, x in (("o", o.detach()), ("dq", leaves[0].grad), ("dk", leaves[1].grad), ("dv", leaves[2].grad)):
         assert (r[name] - x).abs().max() < 1e-12, name
     assert (r["lse"] - torch.logsumexp(s, -1)).abs().max() < 1e-12
+
+
+@pytest.mark.parametrize("change", [
+    dict(q=lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)), dict(v=lambda x: x[:, :7]), dict(v=lambda x: x.float()),
+    dict(o=lambda x: x[..., :32]), dict(lse=lambda x: x.transpose(1, 2).contiguous()), dict(lse=lambda x: x.double()), dict(dq=lambda x: x[:, :, :1]),
+    dict(dk=lambda x: x[:, ::2]), dict(dout=lambda x: x.transpose(1, 2).contiguous().transpose(1, 2), strided=True),
+    dict(k=lambda x: x.as_strided(x.shape, (0, 0, 0, 1)), strided=True),
+], ids=lambda c: "+".join(c))
+def test_binding_refuses_tensors_that_do_not_fit(change):
+    """A view that is not told of, a shape or a type that is off: said by the window calls before anything is launched."""
+    x = lambda h: torch.zeros(1, 8, h, 64, dtype=torch.bfloat16)
+    t = dict(q=x(4), k=x(2), v=x(2), o=x(4), lse=torch.zeros(1, 4, 8), dout=x(4), dq=x(4), dk=x(2), dv=x(2))
+    strided = change.pop("strided", False)
+    assert binding.make_params(**t, G=0, strided=strided).problem is None
+    t.update({n: f(t[n]) for n, f in change.items()})
+    p = binding.make_params(**t, G=0, strided=strided)
+    for call in (binding.s2attn_window_fwd, binding.s2attn_window_bwd):
+        with pytest.raises(ValueError, match=next(iter(change)) + " "):
+            call(p, 4, 0)
