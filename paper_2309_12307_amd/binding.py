@@ -169,6 +169,16 @@ def _import_torch():
     return torch
 
 
+def _current_device() -> int:
+    torch = _torch or _import_torch()
+    try:
+        if torch.cuda.is_initialized():
+            return torch._C._cuda_getDevice()
+    except AttributeError:
+        pass
+    return torch.cuda.current_device()
+
+
 def _stream(stream):
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
@@ -323,9 +333,9 @@ def _on_device(p):
         return
     if device < 0:
         raise ValueError("the tensors are not on a GPU")
-    torch = _torch or _import_torch()
-    if torch.cuda.current_device() != device:
-        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    current = _current_device()
+    if current != device:
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{current}")
 
 
 def _whole(p):
