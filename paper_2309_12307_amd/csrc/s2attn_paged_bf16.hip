@@ -4,10 +4,12 @@
 // are read once for all query heads that share them.  Two kinds of workgroup (4 waves) share a launch:
 //   chunk  128 rows of a sequence that has many, and a piece of their keys; a wave owns 32 rows, the waves share the
 //          64-key tiles, staged in LDS.  S^T = K Q^T, online softmax, O^T += V^T P^T as in the forward kernels on contiguous
-//          tensors.  Bound by the matrix unit.
+//          tensors.  Bound by the matrix unit (2048 rows over 32768 keys, H = 32, D = 128: 990 us, 1080 TFLOP/s; D = 64 by the vector
+//          unit, which has twice the exponentials for a product).
 //   few    all rows of a sequence that has 16 or 32, as single tokens have, and a piece of its keys; the waves take different
 //          32-key tiles and meet once, at the end.  Bound by HBM: what counts is bytes on the way, so a wave has a whole tile of
-//          K and V on its way to registers while it works on another, and waits for nobody.
+//          K and V on its way to registers while it works on another, and waits for nobody (two sequences over 100 000 tokens,
+//          e4m3, 32 kv heads: 290 us, 5.7 TB/s; 32 over up to 8192, bf16, 8 kv heads: 86 us and the join 5).
 // Rows that several pieces share leave normalised fp32 partial outputs and their log-sum-exp, which a second kernel joins.
 //
 // P is rounded to bf16 for the second product (as everywhere in this library); the row sum adds the unrounded P, and

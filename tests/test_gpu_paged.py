@@ -49,6 +49,51 @@ def test_batches(n, dtype, cache):
         b.check(*b.attend(window, sinks, workspace=3 * piece + 100, max_kv=64), want)   # a max_kv that is off
 
 
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("B", [65, 300])
+def test_many_sequences(B, rows, dtype, cache):
+    """More sequences than a wave has lanes, one in ten an empty slot, written, attended and read."""
+    gen = torch.Generator().manual_seed(B + rows)
+    draw = lambda n: int(torch.randint(n, (1,), generator=gen))
+    lens = [(0, 0) if draw(10) == 0 else (1 + draw(rows), 40 + draw(90)) for _ in range(B)]
+    b = Batch(lens, 2, 1, 64, 16, dtype, cache, seed=B, before=1, behind=2)
+    b.check(*b.attend(), b.reference())
+    b.check(*b.attend(30, 2), b.reference(30, 2))
+    k, v = b.k.cuda(), b.v.cuda()
+    binding.s2attn_cache_write(b.params(k=k, v=v))
+    back = [torch.full_like(x, 5.0) for x in (k, v)]
+    binding.s2attn_cache_read(b.params(k=back[0], v=back[1]))
+    torch.cuda.synchronize()
+    own = b.own.cuda()
+    for x, y in zip((b.k, b.v), back):
+        want = x
+        if cache == "e4m3":
+            values, e = ref.quantise(x)
+            want = (values * 2.0 ** (e.double() - 127)[..., None]).to(x.dtype)
+        assert torch.equal(y[own].cpu(), want[b.own]) and (y[~own] == 5).all()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 5)])
+def test_more_rows_than_tokens(window, sinks, dtype, cache):
+    """Rows at negative positions see nothing, in every kind of workgroup."""
+    b = Batch([(300, 100), (150, 149), (9, 3), (40, 0), (1, 0)], 4, 4, 128, 16, dtype, cache, seed=7)
+    want = b.reference(window, sinks)
+    assert torch.isinf(want["lse"][:, :200]).all()
+    b.check(*b.attend(window, sinks), want)
+    b = Batch([(1, 0), (12, 5)], 4, 2, 64, 8, dtype, cache, seed=8)
+    b.check(*b.attend(window, sinks), b.reference(window, sinks))
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_many_query_heads_of_one_kv_head(dtype, cache):
+    b = Batch([(1, 200), (0, 0), (1, 31)], 128, 1, 64, 16, dtype, cache, seed=3)
+    b.check(*b.attend(), b.reference())
+    b = Batch([(3, 200), (1, 90)], 96, 1, 128, 16, dtype, cache, seed=4)
+    b.check(*b.attend(50, 1), b.reference(50, 1))
+
+
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 @pytest.mark.parametrize("page", [16, 40])
 def test_long_chunk(cache, page):
