@@ -76,12 +76,13 @@ struct Plan {
 Plan plan(const s2attn_paged_params* p, bool by16) {
   Plan x{};
   const long long r = p->H / p->Hkv, rows = p->T * r, seqs = std::max(1, std::min(p->B, p->T));
-  // One token a sequence (as far as T and B tell): all go to `few`, which takes any number of rows, by turns of 16 or 32.  Where
-  // some have more, those of up to 16 or 32 rows (fp32: 64, in turns) go there and the others to `chunk`.  us, all in `chunk` and all in
-  // `few`, 4000 keys, D = 128: fp32, one sequence of 16 rows 35.8 and 19.9, of 64 65.9 and 57.2, eight of 16 78 and 56; bf16, one of
-  // 16 15.2 and 14.6, of 48 20.7 and 24.4; one token of 32 sequences, H = 32, bf16 290 and 272, 16 over 30 000 keys, e4m3 558 and 300.
-  const bool f32 = p->dtype == S2ATTN_F32;
-  const long long most_few = f32 ? 64 : 32;
+  // One token a sequence (as far as T and B tell), of up to 16 rows (e4m3 32 in two blocks, fp32 64 in turns): all go to `few`, which takes
+  // any number of rows, by turns.  Where some have more, those of up to 16 rows (fp32 64) go there and the others to `chunk`.  us, all
+  // in `chunk` and all in `few`, 4000 keys, D = 128: fp32, one sequence of 16 rows 35.8 and 19.9, of 64 65.9 and 57.2, eight of 16 78 and
+  // 56; bf16, one of 16 15.2 and 14.6, of 24 15.6 and 15.9, eight of 20 30.5 and 43.6; e4m3, one of 24 20.4 and 15.4, eight of 20 32 and
+  // 39; one token of 32 sequences, H = 32, bf16 290 and 272, 16 over 30 000 keys, e4m3 558 and 300.
+  const bool f32 = p->dtype == S2ATTN_F32, e4m3 = p->cache_dtype == S2ATTN_E4M3;
+  const long long most_few = f32 ? 64 : e4m3 ? 32 : 16;
   x.nq = 1;
   if ((p->T <= p->B && r <= most_few) || rows <= most_few) {
     x.few = true;
@@ -90,8 +91,7 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   } else {
     x.chunk = true;
     x.few = p->B > 1;
-    if (!f32 && rows > 16 * seqs) x.nq = 2;
-    x.few_rows = !x.few ? 0 : f32 ? 64 : 16 * x.nq;
+    x.few_rows = !x.few ? 0 : f32 ? 64 : 16;
   }
   const long long most = (long long)p->table_cols * p->page_size;
   long long keys = p->max_kv > 0 ? std::min<long long>(p->max_kv, most) : most;

@@ -6,7 +6,7 @@
 //          64-key tiles, staged in LDS.  S^T = K Q^T, online softmax, O^T += V^T P^T as in the forward kernels on contiguous
 //          tensors.  Bound by the matrix unit (2048 rows over 32768 keys, H = 32, D = 128: 990 us, 1080 TFLOP/s; D = 64 by the vector
 //          unit, which has twice the exponentials for a product).
-//   few    all rows of a sequence that has 16 or 32, as single tokens have, and a piece of its keys; the waves take different
+//   few    all rows of a sequence that has up to 16 (e4m3: 32), as single tokens have, and a piece of its keys; the waves take different
 //          32-key tiles and meet once, at the end.  Bound by HBM: what counts is bytes on the way, so a wave has a whole tile of
 //          K and V on its way to registers while it works on another, and waits for nobody (two sequences over 100 000 tokens,
 //          e4m3, 32 kv heads: 290 us, 5.7 TB/s; 32 over up to 8192, bf16, 8 kv heads: 86 us and the join 5).
@@ -769,37 +769,33 @@ __global__ void __launch_bounds__(256, 2) paged_few_kernel(PArgs a, int first_bl
   few_workgroup<D, E4M3, BY16, NQ>(a, first_block + block_id(), smem);
 }
 
-template <int D, bool E4M3, bool BY16, int NQ>
+template <int D, bool E4M3, bool BY16>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_both_kernel(PArgs a, int first_block) {
-  __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D> > kFewBytes<D, NQ> ? kChunkBytes<D> : kFewBytes<D, NQ>];
+  __shared__ __attribute__((aligned(1024))) char smem[kChunkBytes<D> > kFewBytes<D, 1> ? kChunkBytes<D> : kFewBytes<D, 1>];
   __shared__ int flags[4];
   const int block = first_block + block_id();
   if (block < a.chunk_blocks)   // the long chains first: 62 us, the others first 72 (16 sequences of 1 to 600 rows, window 4096)
     chunk_workgroup<D, E4M3, BY16>(a, block, smem, flags);
   else
-    few_workgroup<D, E4M3, BY16, NQ>(a, block - a.chunk_blocks, smem);
+    few_workgroup<D, E4M3, BY16, 1>(a, block - a.chunk_blocks, smem);
 }
 
-template <int D, bool E4M3, bool BY16, int NQ>
-int launch_few(const PArgs& a, hipStream_t st) {
-  return launch_blocks(paged_few_kernel<D, E4M3, BY16, NQ>, a.B * a.Hkv * a.few.splits, 256, st, a);
-}
-template <int D, bool E4M3, bool BY16, int NQ>
-int launch_both(const PArgs& a, hipStream_t st) {
-  return launch_blocks(paged_both_kernel<D, E4M3, BY16, NQ>, a.chunk_blocks + a.B * a.Hkv * a.few.splits, 256, st, a);
-}
 template <int D, bool E4M3, bool BY16>
 int launch_t(const PArgs& a, int nq, hipStream_t st) {
-  if (a.chunk_blocks == 0) return nq == 1 ? launch_few<D, E4M3, BY16, 1>(a, st) : launch_few<D, E4M3, BY16, 2>(a, st);
+  const int few = a.B * a.Hkv * a.few.splits;
+  if (a.chunk_blocks == 0) {
+    if constexpr (E4M3)
+      if (nq == 2) return launch_blocks(paged_few_kernel<D, E4M3, BY16, 2>, few, 256, st, a);
+    return launch_blocks(paged_few_kernel<D, E4M3, BY16, 1>, few, 256, st, a);
+  }
   if constexpr (D == 128 && BY16) {
     if (a.chunk_rows == 256) {
       const int rc = launch_blocks(paged_long_kernel<E4M3>, a.chunk_blocks, 512, st, a);
-      if (rc != 0 || a.few_rows == 0) return rc;
-      return nq == 1 ? launch_few<D, E4M3, BY16, 1>(a, st) : launch_few<D, E4M3, BY16, 2>(a, st);
+      return rc != 0 || a.few_rows == 0 ? rc : launch_blocks(paged_few_kernel<D, E4M3, BY16, 1>, few, 256, st, a);
     }
   }
   if (a.few_rows == 0) return launch_blocks(paged_chunk_kernel<D, E4M3, BY16>, a.chunk_blocks, 256, st, a);
-  return nq == 1 ? launch_both<D, E4M3, BY16, 1>(a, st) : launch_both<D, E4M3, BY16, 2>(a, st);
+  return launch_blocks(paged_both_kernel<D, E4M3, BY16>, a.chunk_blocks + few, 256, st, a);
 }
 template <int D, bool E4M3>
 int launch_pages(const PArgs& a, int nq, hipStream_t st) {
