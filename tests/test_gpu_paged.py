@@ -266,3 +266,28 @@ def test_two_graphs_share_a_workspace():
         graphs[i].replay()
         torch.cuda.synchronize()
         assert torch.equal(kw[i]["o"], outs[i][0]) and torch.equal(kw[i]["lse"], outs[i][1]), i
+
+
+def test_two_calls_at_once():
+    """Two steps on two streams, each with its own workspace: the bits of the same steps one after the other."""
+    batches = [Batch([(1, 6000), (40, 3000), (1, 50)], 8, 2, 128, 16, "bf16", "e4m3", seed=31), Batch(MIXED, 8, 2, 64, 16, "f32", "f32", seed=32)]
+    calls = []
+    for b in batches:
+        kw = dict(q=b.q.cuda(), o=torch.empty_like(b.q, device="cuda"), lse=torch.empty(8, b.T, device="cuda"))
+        ws = torch.empty(binding.paged_workspace_bytes(b.params(**kw)), dtype=torch.uint8, device="cuda")
+        calls.append((b.params(workspace=ws, **kw), kw, ws))
+    want = []
+    for p, kw, _ in calls:
+        binding.s2attn_paged_fwd(p)
+        torch.cuda.synchronize()
+        want.append((kw["o"].clone(), kw["lse"].clone()))
+        kw["o"].fill_(float("nan"))
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (p, _, _), s in zip(calls, streams):
+            binding.s2attn_paged_fwd(p, stream=s)
+    torch.cuda.synchronize()
+    for b, (_, kw, _), (o, lse) in zip(batches, calls, want):
+        own = b.own.cuda()
+        assert torch.equal(kw["o"][own], o[own]) and torch.equal(kw["lse"][:, own], lse[:, own])
