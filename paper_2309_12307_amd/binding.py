@@ -235,9 +235,9 @@ def make_params(q, k, v, o, lse, G, dout=None, dq=None, dk=None, dv=None, worksp
     else:
         B, N, H, Hkv, D = dims
     p = S2AttnParams()
-    p.device = None if isinstance(q, int) else _device_of(q)
-    p.problem = None if isinstance(q, int) else _problem_of(
-        q, dict(k=k, v=v, dk=dk, dv=dv), dict(o=o, dout=dout, dq=dq), lse, (B, N, H, Hkv, D), strided)
+    tensors = not (q is None or isinstance(q, int))   # (a block for a size alone may have neither)
+    p.device = _device_of(q) if tensors else None
+    p.problem = _problem_of(q, dict(k=k, v=v, dk=dk, dv=dv), dict(o=o, dout=dout, dq=dq), lse, (B, N, H, Hkv, D), strided) if tensors else None
     p.q, p.k, p.v, p.o, p.lse = _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse)
     p.dout, p.dq, p.dk, p.dv = _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv)
     p.workspace = _ptr(workspace)
