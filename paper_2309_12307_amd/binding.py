@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import weakref
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("S2ATTN_LIB", os.path.join(_HERE, "libs2attn.so"))
@@ -45,6 +46,8 @@ class S2AttnParams(ctypes.Structure):
         ("dk_strides", ctypes.c_longlong * 3), ("dv_strides", ctypes.c_longlong * 3),
         ("heads_total", ctypes.c_int), ("head_offset", ctypes.c_int), ("bwd_algo", ctypes.c_int),
     ]
+    # what the window calls go by: the device of the tensors, what is wrong with them, and those not looked at yet
+    device = problem = tensors = None
 
 
 class S2AttnPagedParams(ctypes.Structure):
@@ -235,9 +238,15 @@ def make_params(q, k, v, o, lse, G, dout=None, dq=None, dk=None, dv=None, worksp
     else:
         B, N, H, Hkv, D = dims
     p = S2AttnParams()
-    tensors = not (q is None or isinstance(q, int))   # (a block for a size alone may have neither)
-    p.device = _device_of(q) if tensors else None
-    p.problem = _problem_of(q, dict(k=k, v=v, dk=dk, dv=dv), dict(o=o, dout=dout, dq=dq), lse, (B, N, H, Hkv, D), strided) if tensors else None
+    if q is not None and not isinstance(q, int):   # (a block for a size alone may have neither)
+        tensors = (q, k, v, o, lse, dout, dq, dk, dv)
+        if G == 0:   # for the window calls
+            p.device, p.problem = _device_of(q), _problem_of(*tensors, (B, N, H, Hkv, D), strided)
+        else:        # they may get any block: a look at the tensors that are still there then, none for the others' calls
+            try:
+                p.tensors = list(map(weakref.ref, tensors[:5] if dout is None else tensors)), strided
+            except TypeError:   # addresses among them
+                p.tensors = [x if x is None or isinstance(x, int) else weakref.ref(x) for x in tensors], strided
     p.q, p.k, p.v, p.o, p.lse = _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse)
     p.dout, p.dq, p.dk, p.dv = _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv)
     p.workspace = _ptr(workspace)
@@ -256,10 +265,10 @@ def make_params(q, k, v, o, lse, G, dout=None, dq=None, dk=None, dv=None, worksp
     return p
 
 
-def _problem_of(q, like_k, like_q, lse, dims, strided):
+def _problem_of(q, k, v, o, lse, dout, dq, dk, dv, dims, strided):
     """What is wrong with a block's tensors (None: nothing): s2attn_window_fwd and s2attn_window_bwd refuse it."""
     B, N, H, Hkv, D = dims
-    for shape, tensors in (((B, N, Hkv, D), like_k), ((B, N, H, D), dict(like_q, q=q))):
+    for shape, tensors in (((B, N, Hkv, D), dict(k=k, v=v, dk=dk, dv=dv)), ((B, N, H, D), dict(o=o, dout=dout, dq=dq, q=q))):
         for name, t in tensors.items():
             if t is None or isinstance(t, int):
                 continue
@@ -339,7 +348,14 @@ def _on_device(p):
 
 
 def _whole(p):
-    if getattr(p, "problem", None):
+    if p.tensors is not None:
+        refs, strided = p.tensors
+        tensors = [x() if isinstance(x, weakref.ref) else x for x in refs]
+        tensors += [None] * (9 - len(tensors))   # (a forward's has no gradients)
+        if tensors[0] is not None:
+            p.device, p.problem = _device_of(tensors[0]), _problem_of(*tensors, (p.B, p.N, p.H, p.Hkv, p.D), strided)
+        p.tensors = None
+    if p.problem:
         raise ValueError(p.problem)
     _on_device(p)
 
