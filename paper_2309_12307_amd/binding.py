@@ -239,7 +239,7 @@ def make_params(q, k, v, o, lse, G, dout=None, dq=None, dk=None, dv=None, worksp
         B, N, H, Hkv, D = dims
     p = S2AttnParams()
     if q is not None and not isinstance(q, int):   # (a block for a size alone may have neither)
-        tensors = (q, k, v, o, lse, dout, dq, dk, dv)
+        tensors = (q, k, v, o, lse, dout, dq, dk, dv, workspace)
         if G == 0:   # for the window calls
             p.device, p.problem = _device_of(q), _problem_of(*tensors, (B, N, H, Hkv, D), strided)
         else:        # they may get any block: a look at the tensors that are still there then, none for the others' calls
@@ -265,7 +265,7 @@ def make_params(q, k, v, o, lse, G, dout=None, dq=None, dk=None, dv=None, worksp
     return p
 
 
-def _problem_of(q, k, v, o, lse, dout, dq, dk, dv, dims, strided):
+def _problem_of(q, k, v, o, lse, dout, dq, dk, dv, workspace, dims, strided):
     """What is wrong with a block's tensors (None: nothing): s2attn_window_fwd and s2attn_window_bwd refuse it."""
     B, N, H, Hkv, D = dims
     for shape, tensors in (((B, N, Hkv, D), dict(k=k, v=v, dk=dk, dv=dv)), ((B, N, H, D), dict(o=o, dout=dout, dq=dq, q=q))):
@@ -282,6 +282,8 @@ def _problem_of(q, k, v, o, lse, dout, dq, dk, dv, dims, strided):
     if not (lse is None or isinstance(lse, int)):
         if lse.shape != (B, H, N) or lse.element_size() != 4 or not lse.is_floating_point() or not lse.is_contiguous() or lse.device != q.device:
             return f"lse must be a contiguous float32 {(B, H, N)} on q's device"
+    if not (workspace is None or isinstance(workspace, int)) and not (workspace.is_contiguous() and workspace.device == q.device):
+        return "workspace must be contiguous on q's device"
     return None
 
 
@@ -351,7 +353,7 @@ def _whole(p):
     if p.tensors is not None:
         refs, strided = p.tensors
         tensors = [x() if isinstance(x, weakref.ref) else x for x in refs]
-        tensors += [None] * (9 - len(tensors))   # (a forward's has no gradients)
+        tensors += [None] * (10 - len(tensors))   # (a forward's has no gradients)
         if tensors[0] is not None:
             p.device, p.problem = _device_of(tensors[0]), _problem_of(*tensors, (p.B, p.N, p.H, p.Hkv, p.D), strided)
         p.tensors = None
@@ -467,6 +469,8 @@ def make_paged_params(row_start, kv_len, page_table, k_cache, v_cache, k_exp=Non
             setattr(p, name, at)
             setattr(p, name + "_strides", strides)
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
         p.workspace, p.workspace_bytes = workspace.data_ptr() or None, workspace.numel() * workspace.element_size()
     p.window, p.sinks, p.max_kv, p.scale = window, sinks, max_kv, scale
     return p

@@ -54,3 +54,18 @@ def test_tensors_beside_addresses_and_tensors_that_are_gone():
     del t["v"]
     with pytest.raises(ValueError, match="not on a GPU"):
         binding.s2attn_window_fwd(p, 4)
+
+
+@pytest.mark.parametrize("G", [0, 4])
+@pytest.mark.parametrize("workspace", [torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 21, dtype=torch.uint8)[::2],
+                                       torch.zeros(1 << 20, dtype=torch.uint8, device="meta")], ids=["expanded", "strided", "elsewhere"])
+def test_workspaces_that_are_not_there(workspace, G):
+    """Fewer bytes than elements, or bytes of another device: the kernels would write outside."""
+    t = tensors()
+    p = binding.make_params(**t, workspace=workspace, G=G)
+    with pytest.raises(ValueError, match="workspace must be contiguous on q's device"):
+        binding.s2attn_window_bwd(p, 4, 0)
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    cache, q = torch.zeros(6, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(5, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="workspace must be contiguous|one device"):
+        binding.make_paged_params(i32(2), i32(1), i32(1, 3), cache, cache, q=q, o=q, workspace=workspace)
