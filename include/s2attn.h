@@ -237,6 +237,9 @@ S2ATTN_API int s2attn_window_bwd(const s2attn_params* p, int window, int sinks, 
  *   - rows that belong to no sequence (before row_start[0], from row_start[B] on) are left as they are;
  *   - positions from table_cols * page_size on and pages outside [0, pages) do not exist: nothing is written there, they are read
  *     as zeros, and their keys are invisible.  Memory of a page behind kv_len is never read: it may hold anything;
+ *   - nor are keys that no row of their sequence in the call sees, those between the sinks and the first row's window: pages there
+ *     may have been given up, and the table may still name them.  Keys that some of the sequence's rows see have to be finite: one that
+ *     another row does not see (a later token, one before its window) is multiplied by zero, not left out;
  *   - a row that sees no key gets o = 0 and lse = -infinity (also where a sequence has more rows than cached tokens: rows at
  *     negative positions are not written to the cache, are read as zeros and see nothing).
  * Sequences may share pages (a common prefix).  Two rows of one s2attn_cache_write must not name the same place: which of

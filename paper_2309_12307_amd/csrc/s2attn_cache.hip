@@ -184,7 +184,8 @@ __global__ void __launch_bounds__(256) cache_kernel(PArgs a, int tokens, Div by_
   if (tokens == 1) {
     const SeqRows sr = find_rows<-1>(a, t0, lane);
     const bool in = sr.b >= 0 && t0 >= sr.s0 && t0 < sr.s0 + sr.n;
-    const CacheRow one = in ? cache_row(a, sr.b, sr.kv - sr.n + (t0 - sr.s0), sr.keys) : CacheRow{-1, 0};
+    const int p = sr.kv - sr.n + (t0 - sr.s0);
+    const CacheRow one = cache_row(a, sr.b, p, in && p >= 0 && p < sr.keys);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) { at[s] = one; mine[s] = in; }
   } else {
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(256) cache_kernel(PArgs a, int tokens, Div by_
         if (in && t[s] == t0 + u) { b[s] = sr.b; pos[s] = sr.kv - sr.n + (t0 + u - sr.s0); keys[s] = sr.keys; mine[s] = true; }
     }
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) at[s] = cache_row(a, b[s], pos[s], keys[s]);
+    for (int s = 0; s < kSteps; ++s) at[s] = cache_row(a, b[s], pos[s], pos[s] >= 0 && pos[s] < keys[s]);
   }
   u32x4 y[kSteps];
   float scale[kSteps];

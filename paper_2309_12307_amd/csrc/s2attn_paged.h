@@ -121,13 +121,20 @@ __device__ __forceinline__ Piece pieces_of(const PSet& set, int total) {
   return x;
 }
 
-// The cache row of key position j: page number (-1: none) and place in the page.
+// Of the keys before `end`, the rows of a tile from position p_lo on see all but those between the sinks and their windows: pages
+// there may have been given up, and their memory may be anything.
+__device__ __forceinline__ bool is_seen(const PArgs& a, int p_lo, int end, int j) {
+  const int lo = a.window > 0 ? p_lo - a.window + 1 : 0;
+  return (j < end) & ((j >= lo) | (j < a.sinks));
+}
+
+// The cache row of key position j, if it is wanted: page number (-1: none) and place in the page.
 struct CacheRow {
   int page, at;
 };
-__device__ __forceinline__ CacheRow cache_row(const PArgs& a, int b, int j, int end) {
+__device__ __forceinline__ CacheRow cache_row(const PArgs& a, int b, int j, bool wanted) {
   CacheRow x{-1, 0};
-  if (j >= 0 && j < end) {
+  if (wanted) {
     const int slot = quot(j, a.by_page);
     x.at = j - slot * a.page_size;
     const int page = a.table[b * a.table_b + slot];
@@ -155,24 +162,28 @@ __device__ __forceinline__ Groups<N> groups_of(const PArgs& a, int b, int j0) {
   for (int g = 0; g < N; ++g) x.page[g] = a.table[b * a.table_b + quot(min(j0 + 16 * g, a.max_keys - 1), a.by_page)];
   return x;
 }
-// The place in its page of key j0, and a bit for each key of the tile that exists.
+// The place in its page of key j0.
 __device__ __forceinline__ int place_of(const PArgs& a, int j0) { return j0 - quot(j0, a.by_page) * a.page_size; }
 // Bytes from a cache's first row (of a head) to place `at` of page `page`, all factors below 2^32 where a.by16.
 __device__ __forceinline__ uint64_t group_off(int page, int at, long long page_bytes, long long token_bytes) {
   return (uint64_t)(uint32_t)page * (uint32_t)page_bytes + (uint32_t)at * (uint32_t)token_bytes;
 }
 template <int N>
-__device__ __forceinline__ uint64_t seen_of(const PArgs& a, const Groups<N>& x, int j0, int end) {
+__device__ __forceinline__ uint64_t bits_below(int n) { return n >= 16 * N ? ~0ull : n <= 0 ? 0 : (1ull << n) - 1; }
+// A bit for each of the 16 N keys from j0 on that exists and that some row of the tile sees (is_seen).
+template <int N>
+__device__ __forceinline__ uint64_t seen_of(const PArgs& a, const Groups<N>& x, int p_lo, int end, int j0) {
   uint64_t seen = 0;
 #pragma unroll
   for (int g = 0; g < N; ++g)
     if ((unsigned)x.page[g] < (unsigned)a.pages) seen |= 0xffffull << (16 * g);
-  const int left = end - j0;   // keys before `end`
-  return left >= 16 * N ? seen : left <= 0 ? 0 : seen & ((1ull << left) - 1);
+  seen &= bits_below<N>(end - j0);
+  if (a.window > 0 && j0 < p_lo - a.window + 1) seen &= ~bits_below<N>(p_lo - a.window + 1 - j0) | bits_below<N>(a.sinks - j0);
+  return seen;
 }
 
 // Tiles [from, n1) of TK keys of a walk lie on pages that exist and before `end`: their loads need no test.  The tiles of the sinks and
-// the first of the window stay out: pages between may have been given up.  The whole workgroup of THREADS looks.
+// the first of the window stay out: not all of their keys are seen.  The whole workgroup of THREADS looks.
 struct Plain {
   int from, to;
 };

@@ -154,12 +154,12 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
   auto look_up = [&](int n) __attribute__((always_inline)) {
     Ahead x;
     if constexpr (BY16) x.page = groups_of<1>(a, b, kt.tile(min(n, n1 - 1)) * kKeys + 16 * w).page[0];
-    else x.row = n < n1 ? cache_row(a, b, kt.tile(n) * kKeys + lane, kt.end) : CacheRow{-1, 0};
+    else x.row = cache_row(a, b, kt.tile(n) * kKeys + lane, n < n1 && is_seen(a, p_lo, kt.end, kt.tile(n) * kKeys + lane));
     return x;
   };
   u32x4 k8[2][kPass], v8[2][kPass];                             // e4m3: two tiles on their way
   float ks8[2][kPass], vs8[2][kPass];
-  // Starts the loads of tile n; a bit for each key that exists.
+  // Starts the loads of tile n; a bit for each key that exists and that some row sees.
   auto issue = [&](const Ahead& x, int n, int stage) __attribute__((always_inline)) {
     const uint32_t dst = smem_base + stage * 2 * kTileBytes + w * kPass * 1024;
     const uint64_t zero = zero_address();
@@ -169,7 +169,7 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
       const uint64_t vb = v_head + group_off(x.page, at, a.vc_p * kEsz, a.vc_t * kEsz);
       uint64_t seen = ~0ull;
       const bool all = n >= plain.from && n < plain.to;
-      if (!all) seen = seen_of<4>(a, groups_of<4>(a, b, j0), j0, n < n1 ? kt.end : 0);
+      if (!all) seen = n < n1 ? seen_of<4>(a, groups_of<4>(a, b, j0), p_lo, kt.end, j0) : 0;
       const uint32_t mine = (uint32_t)(seen >> (16 * w)) & 0xffffu;
 #pragma unroll
       for (int p = 0; p < kPass; ++p) {
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
     const bool all = n0 + n >= plain.from && n0 + n < plain.to;
     seen_a = seen_b;
     seen_b = ~0ull;
-    if (!all) seen_b = seen_of<4>(a, groups_of<4>(a, b, j0), j0, kt.end);
+    if (!all) seen_b = seen_of<4>(a, groups_of<4>(a, b, j0), p_lo, kt.end, j0);
     const uint32_t dst = smem_base + stage * kStageBytes + 8 * w * kRowBytes;
     const uint64_t zero = zero_address();
     const uint64_t kb = k_head + group_off(page, at, a.kc_p * kEsz, a.kc_t * kEsz);
@@ -474,7 +474,7 @@ struct FewTile {
   static constexpr int N = D / (E4M3 ? 64 : 32);   // pieces of a key and lane
   u32x4 k[2][N], v[2][N];
   float ks[2], vs[2];                              // e4m3: scales
-  uint32_t seen;                                   // a bit for each key that exists
+  uint32_t seen;                                   // a bit for each key that exists and that some row sees
 };
 
 template <int D, bool E4M3, bool BY16, int NQ>
@@ -521,7 +521,10 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
     };
     auto rows_of = [&](int n, CacheRow (&x)[2]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) x[kb] = n < n1 ? cache_row(a, b, kt.tile(n) * TK + 16 * kb + c16, kt.end) : CacheRow{-1, 0};
+      for (int kb = 0; kb < 2; ++kb) {
+        const int j = kt.tile(n) * TK + 16 * kb + c16;
+        x[kb] = cache_row(a, b, j, n < n1 && is_seen(a, p_lo, kt.end, j));
+      }
     };
     auto look_up = [&](int n, Ahead& x) __attribute__((always_inline)) {
       if constexpr (BY16) x.groups = groups_of<2>(a, b, kt.tile(max(min(n, n1 - 1), 0)) * TK);
@@ -532,7 +535,7 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
       int j0 = 0;
       if constexpr (BY16) {
         j0 = kt.tile(max(min(n, n1 - 1), 0)) * TK;
-        t.seen = (uint32_t)seen_of<2>(a, x.groups, j0, n < n1 ? kt.end : 0);
+        t.seen = n < n1 ? (uint32_t)seen_of<2>(a, x.groups, p_lo, kt.end, j0) : 0;
       } else {
         t.seen = ((uint32_t)__builtin_amdgcn_ballot_w64(x.row[0].page >= 0) & 0xffffu) |
                  ((uint32_t)__builtin_amdgcn_ballot_w64(x.row[1].page >= 0) << 16);

@@ -49,9 +49,10 @@ __device__ __forceinline__ void chunk_f32_workgroup(const PArgs& a, int block, c
   const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz;
   const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
   const uint32_t base = lds_addr(smem);
-  // every wave looks up the 32 keys of a tile, twice; `seen` has a bit for each that exists
+  // every wave looks up the 32 keys of a tile, twice; `seen` has a bit for each that exists and that some row sees
   auto look_up = [&](int n) __attribute__((always_inline)) {
-    return n < n1 ? cache_row(a, b, kt.tile(n) * kTile + (lane & 31), kt.end) : CacheRow{-1, 0};
+    const int j = kt.tile(n) * kTile + (lane & 31);
+    return cache_row(a, b, j, n < n1 && is_seen(a, p_lo, kt.end, j));
   };
   auto seen_of = [&](const CacheRow& x) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_ballot_w64(x.page >= 0); };
 
@@ -245,7 +246,8 @@ __device__ __forceinline__ void few_f32_workgroup(const PArgs& a, int block, flo
     if (split > 0 && n0 >= n1) continue;
 
     auto look_up = [&](int n) __attribute__((always_inline)) {
-      return n < n1 ? cache_row(a, b, kt.tile(n) * TK + c16, kt.end) : CacheRow{-1, 0};
+      const int j = kt.tile(n) * TK + c16;
+      return cache_row(a, b, j, n < n1 && is_seen(a, p_lo, kt.end, j));
     };
     auto load = [&](T& t, const CacheRow& x) __attribute__((always_inline)) {
       t.seen = (uint32_t)__builtin_amdgcn_ballot_w64(x.page >= 0) & 0xffffu;
