@@ -4,6 +4,8 @@
 // Nothing that these kernels read from the device is trusted with an address: row_start is clamped to [0, T], key positions
 // stay below table_cols * page_size, and a page number outside [0, pages) stands for no page (its keys are invisible).
 #pragma once
+#include <type_traits>
+
 #include "s2attn_device.h"
 
 namespace s2 {
@@ -11,7 +13,7 @@ namespace s2 {
 // How the work of a launch, or of a part of it, is dealt out.
 struct PSet {
   int splits, min_tiles;                       // most pieces the keys of a row tile are cut into; fewest key tiles of one
-  int n_tiles;                                 // row tiles (chunk), sequences (few)
+  int n_tiles;                                 // row tiles (chunk), sequences or tokens (few)
   Div by_tiles, by_groups, by_splits, by_min;  // n_tiles, Hkv * splits, splits, min_tiles
 };
 
@@ -30,9 +32,10 @@ struct PArgs {
   int window, sinks;                           // window 0: every earlier key is visible
   PSet chunk, few;                             // sequences of more than few_rows (row, head of the kv head) pairs, and the others
   int few_rows, chunk_rows;                    // chunk_rows: of a row tile of `chunk`
+  int few_tokens;                              // `few` deals out so many tokens of a sequence at a time (0: a sequence's whole)
   int by16;                                    // pages of a multiple of 16 tokens, 16 rows of one within 31-bit offsets
   int chunk_blocks;                            // blocks of `chunk`; those of `few` follow
-  Div by_r, by_page, by_Hkv;
+  Div by_r, by_page, by_Hkv, by_few_tokens;
   float scale_log2;
 };
 
@@ -58,17 +61,17 @@ __device__ __forceinline__ SeqRows seq_rows(const PArgs& a, int b) {
 // tiles of 2^SHIFT (token, query head of the kv head) pairs, of which a sequence owns those from
 // (row_start[b] * r >> SHIFT) + b on: at least as many as it needs, and no running sum is needed to place them.
 // The whole wave calls it and has one answer: up to 64 sequences are looked at together, everything about them read at once;
-// more are narrowed down by looking at every 64th part first.  Where row_start falls, the answer is some sequence.
+// more are narrowed down by looking at every 64th part first.  Where row_start falls, the answer is some sequence.  lo, hi: only
+// sequences lo .. hi - 1 are looked at.
 template <int SHIFT>
 __device__ __forceinline__ int first_tile(const PArgs& a, int s0, int b) { return (int)((unsigned)(s0 * a.r) >> SHIFT) + b; }
 template <int SHIFT>
-__device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane) {
+__device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane, int lo, int hi) {
   auto before = [&](int start, int i) __attribute__((always_inline)) {
     const int s0 = min(max(start, 0), a.T);
     if constexpr (SHIFT < 0) return s0 <= id;
     else return first_tile<SHIFT>(a, s0, i) <= id;
   };
-  int lo = 0, hi = a.B;
   while (hi - lo > 64) {
     const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
     const int m = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && before(a.row_start[min(i, hi - 1)], i)));
@@ -85,6 +88,35 @@ __device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane) {
   s.kv = max(__builtin_amdgcn_readlane(kv, max(l, 0)), 0);
   s.keys = min(s.kv, a.max_keys);
   return s;
+}
+template <int SHIFT>
+__device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane) { return find_rows<SHIFT>(a, id, lane, 0, a.B); }
+
+// Rows i0 .. i1 - 1 of a sequence's (token, query head of the kv head) pairs: those of a workgroup of `few`, by turns where it holds fewer.
+struct FewRows {
+  SeqRows sr;
+  int i0, i1;
+};
+// The rows of unit u: a sequence of up to few_rows rows, or, from the u-th token on, the next few_tokens ones of its sequence.  The latter
+// where there are no more tokens than sequences, as in a step of single tokens: unit u is then of sequence u or, where some have no row,
+// of one of the next, which are looked at first.  A sequence that has several tokens after all has workgroups for all of them.
+__device__ __forceinline__ bool few_rows_of(const PArgs& a, int u, int lane, FewRows& x) {
+  if (a.few_tokens == 0) {
+    if (u >= a.B) return false;
+    x.sr = seq_rows(a, u);
+    x.i0 = 0;
+    x.i1 = wave_uniform(x.sr.n * a.r);
+    return x.i1 <= a.few_rows;
+  }
+  if (u >= a.T) return false;
+  const int near = min(u + 64, a.B);   // (u is less than B too)
+  x.sr = find_rows<-1>(a, u, lane, u, near);
+  if (x.sr.b < 0 || (x.sr.b == near - 1 && near < a.B)) x.sr = find_rows<-1>(a, u, lane);
+  const int tok = u - x.sr.s0, part = quot(max(tok, 0), a.by_few_tokens);
+  if (x.sr.b < 0 || tok < 0 || tok >= x.sr.n || tok != part * a.few_tokens) return false;
+  x.i0 = wave_uniform(tok * a.r);
+  x.i1 = wave_uniform(min(tok + a.few_tokens, x.sr.n) * a.r);
+  return true;
 }
 
 // Block -> (row tile, kv head, split).  Blocks of one (kv head, split) read the same keys: whole such groups go to an XCD
@@ -168,17 +200,19 @@ __device__ __forceinline__ int place_of(const PArgs& a, int j0) { return j0 - qu
 __device__ __forceinline__ uint64_t group_off(int page, int at, long long page_bytes, long long token_bytes) {
   return (uint64_t)(uint32_t)page * (uint32_t)page_bytes + (uint32_t)at * (uint32_t)token_bytes;
 }
-template <int N>
-__device__ __forceinline__ uint64_t bits_below(int n) { return n >= 16 * N ? ~0ull : n <= 0 ? 0 : (1ull << n) - 1; }
 // A bit for each of the 16 N keys from j0 on that exists and that some row of the tile sees (is_seen).
 template <int N>
-__device__ __forceinline__ uint64_t seen_of(const PArgs& a, const Groups<N>& x, int p_lo, int end, int j0) {
-  uint64_t seen = 0;
+using KeyBits = std::conditional_t<N == 2, uint32_t, uint64_t>;
+template <int N>
+__device__ __forceinline__ KeyBits<N> bits_below(int n) { return n >= 16 * N ? ~KeyBits<N>{0} : n <= 0 ? 0 : (KeyBits<N>{1} << n) - 1; }
+template <int N>
+__device__ __forceinline__ KeyBits<N> seen_of(const PArgs& a, const Groups<N>& x, int p_lo, int end, int j0) {
+  KeyBits<N> seen = 0;
 #pragma unroll
   for (int g = 0; g < N; ++g)
-    if ((unsigned)x.page[g] < (unsigned)a.pages) seen |= 0xffffull << (16 * g);
-  seen &= bits_below<N>(end - j0);
-  if (a.window > 0 && j0 < p_lo - a.window + 1) seen &= ~bits_below<N>(p_lo - a.window + 1 - j0) | bits_below<N>(a.sinks - j0);
+    if ((unsigned)x.page[g] < (unsigned)a.pages) seen |= KeyBits<N>{0xffff} << (16 * g);
+  const int lo = a.window > 0 ? p_lo - a.window + 1 : 0;
+  if (j0 < lo || j0 + 16 * N > end) seen &= bits_below<N>(end - j0) & (~bits_below<N>(lo - j0) | bits_below<N>(a.sinks - j0));
   return seen;
 }
 

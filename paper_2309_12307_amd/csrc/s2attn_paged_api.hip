@@ -70,14 +70,17 @@ struct Plan {
   bool chunk, few;
   int chunk_rows;              // of a row tile of `chunk`
   int nq, few_rows;            // 16-row blocks of a `few` workgroup; the most rows of a sequence that goes there
+  int few_tokens;              // tokens dealt out at a time there, 0: sequences
   int chunk_splits, chunk_min; // pieces, key tiles of a piece at least
   int few_splits, few_min;
 };
 Plan plan(const s2attn_paged_params* p, bool by16) {
   Plan x{};
   const long long r = p->H / p->Hkv, rows = p->T * r, seqs = std::max(1, std::min(p->B, p->T));
-  // One token a sequence (as far as T and B tell), of up to 16 rows (e4m3 32 in two blocks, fp32 64 in turns): all go to `few`, which takes
-  // any number of rows, by turns.  Where some have more, those of up to 16 rows (fp32 64) go there and the others to `chunk`.  us, all
+  // One token a sequence (as far as T and B tell), of up to 16 rows (e4m3 32 in two blocks, fp32 64 in turns): all go to `few`, by as many
+  // tokens as a turn takes: a sequence that has several after all, among empty slots, has workgroups for all of them (256 rows of one
+  // of 256 sequences over 8192 keys, H = 64, Hkv = 8, D = 128: 0.93 ms; by turns of one workgroup to a kv head 16.0; as the only
+  // sequence, in `chunk`, 0.09).  Rows that are few in all go there by turns.  Where some sequences have more, those of up to 16 rows (fp32 64) go there and the others to `chunk`.  us, all
   // in `chunk` and all in `few`, 4000 keys, D = 128: fp32, one sequence of 16 rows 35.8 and 19.9, of 64 65.9 and 57.2, eight of 16 78 and
   // 56; bf16, one of 16 15.2 and 14.6, of 24 15.6 and 15.9, eight of 20 30.5 and 43.6; e4m3, one of 24 20.4 and 15.4, eight of 20 32 and
   // 39; one token of 32 sequences, H = 32, bf16 290 and 272, 16 over 30 000 keys, e4m3 558 and 300.
@@ -88,6 +91,7 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
     x.few = true;
     if (!f32 && (p->T <= p->B ? r : rows) > 16) x.nq = 2;
     x.few_rows = INT_MAX;
+    if (p->T <= p->B) x.few_tokens = std::max(1, 16 * x.nq / (int)r);
   } else {
     x.chunk = true;
     x.few = p->B > 1;
@@ -255,10 +259,12 @@ int s2attn_paged_fwd(const s2attn_paged_params* p, void* stream) {
     return n_tiles * p->Hkv * s.splits;
   };
   a.few_rows = x.few_rows;
+  a.few_tokens = x.few_tokens;
+  a.by_few_tokens = s2::div_by(std::max(1, x.few_tokens));
   a.chunk_rows = x.chunk_rows;
   a.chunk_blocks = set(a.chunk, (int)row_tiles(p, x.chunk_rows), x.chunk_splits, x.chunk_min);
   if (!x.chunk) a.chunk_blocks = 0;
-  set(a.few, p->B, x.few_splits, x.few_min);
+  set(a.few, x.few_tokens > 0 ? p->T : p->B, x.few_splits, x.few_min);
   const int splits = std::max(a.chunk.splits, a.few.splits);
   if (splits > 1) {
     a.part_o = static_cast<float*>(p->workspace);

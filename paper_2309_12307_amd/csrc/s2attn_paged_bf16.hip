@@ -6,8 +6,8 @@
 //          64-key tiles, staged in LDS.  S^T = K Q^T, online softmax, O^T += V^T P^T as in the forward kernels on contiguous
 //          tensors.  Bound by the matrix unit (2048 rows over 32768 keys, H = 32, D = 128: 990 us, 1080 TFLOP/s; D = 64 by the vector
 //          unit, which has twice the exponentials for a product).
-//   few    all rows of a sequence that has up to 16 (e4m3: 32), as single tokens have, and a piece of its keys; the waves take different
-//          32-key tiles and meet once, at the end.  Bound by HBM: what counts is bytes on the way, so a wave has a whole tile of
+//   few    all rows of a sequence that has up to 16 (e4m3: 32), as single tokens have, or as many of its tokens as make that, and a
+//          piece of its keys; the waves take different 32-key tiles and meet once, at the end.  Bound by HBM: what counts is bytes on the way, so a wave has a whole tile of
 //          K and V on its way to registers while it works on another, and waits for nobody (two sequences over 100 000 tokens,
 //          e4m3, 32 kv heads: 290 us, 5.7 TB/s; 32 over up to 8192, bf16, 8 kv heads: 86 us and the join 5).
 // Rows that several pieces share leave normalised fp32 partial outputs and their log-sum-exp, which a second kernel joins.
@@ -485,11 +485,11 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
   const int y = quot(block, a.by_Hkv), c = block - y * a.Hkv;
-  const int b = quot(y, a.few.by_splits), split = y - b * a.few.splits;
-  if (b >= a.B) return;
-  const SeqRows sr = seq_rows(a, b);
-  const int n_rows = uni(sr.n * a.r), p_first = uni(sr.kv - sr.n);
-  if (n_rows > a.few_rows) return;
+  const int unit = quot(y, a.few.by_splits), split = y - unit * a.few.splits;
+  FewRows rows;
+  if (!few_rows_of(a, unit, lane, rows)) return;
+  const SeqRows sr = rows.sr;
+  const int b = sr.b, n_rows = rows.i1, p_first = uni(sr.kv - sr.n);
 
   const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz;
   const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz;
@@ -508,7 +508,7 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
     tr[db] = Tile<D>::off(row, col >> 3) + (col & 7) * 2;
   }
 
-  for (int i0 = 0; i0 < n_rows; i0 += 16 * NQ) {
+  for (int i0 = rows.i0; i0 < n_rows; i0 += 16 * NQ) {
     const int p_lo = uni(p_first + quot(i0, a.by_r)), p_hi = uni(p_first + quot(min(i0 + 16 * NQ, n_rows) - 1, a.by_r));
     const KeyTiles kt = key_tiles<TK>(a.window, a.sinks, p_lo, p_hi, sr.keys);
     const Piece piece = pieces_of(a.few, kt.total);
@@ -535,7 +535,7 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
       int j0 = 0;
       if constexpr (BY16) {
         j0 = kt.tile(max(min(n, n1 - 1), 0)) * TK;
-        t.seen = n < n1 ? (uint32_t)seen_of<2>(a, x.groups, p_lo, kt.end, j0) : 0;
+        t.seen = n < n1 ? seen_of<2>(a, x.groups, p_lo, kt.end, j0) : 0;
       } else {
         t.seen = ((uint32_t)__builtin_amdgcn_ballot_w64(x.row[0].page >= 0) & 0xffffu) |
                  ((uint32_t)__builtin_amdgcn_ballot_w64(x.row[1].page >= 0) << 16);
@@ -750,7 +750,8 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
         if (ch == 0 && a.lse) a.lse[(size_t)h * a.T + t] = lse2 * kLn2;
       }
     }
-    __syncthreads();   // before the next rows' V
+    if constexpr (NQ > 1) return;   // 32 rows at most: no other turn
+    __syncthreads();                // before the next rows' V
   }
 }
 
@@ -785,7 +786,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_both_kernel(PArgs 
 
 template <int D, bool E4M3, bool BY16>
 int launch_t(const PArgs& a, int nq, hipStream_t st) {
-  const int few = a.B * a.Hkv * a.few.splits;
+  const int few = a.few.n_tiles * a.Hkv * a.few.splits;
   if (a.chunk_blocks == 0) {
     if constexpr (E4M3)
       if (nq == 2) return launch_blocks(paged_few_kernel<D, E4M3, BY16, 2>, few, 256, st, a);

@@ -228,17 +228,17 @@ __device__ __forceinline__ void few_f32_workgroup(const PArgs& a, int block, flo
   const int tid = thread_id(), lane = tid & 63, w = uni(tid >> 6);
   const int c16 = lane & 15, q4 = lane >> 4;
   const int y = quot(block, a.by_Hkv), c = block - y * a.Hkv;
-  const int b = quot(y, a.few.by_splits), split = y - b * a.few.splits;
-  if (b >= a.B) return;
-  const SeqRows sr = seq_rows(a, b);
-  const int n_rows = uni(sr.n * a.r), p_first = uni(sr.kv - sr.n);
-  if (n_rows > a.few_rows) return;
+  const int unit = quot(y, a.few.by_splits), split = y - unit * a.few.splits;
+  FewRows rows;
+  if (!few_rows_of(a, unit, lane, rows)) return;
+  const SeqRows sr = rows.sr;
+  const int b = sr.b, n_rows = rows.i1, p_first = uni(sr.kv - sr.n);
   const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz + 16 * q4;
   const uint64_t v_head = reinterpret_cast<uint64_t>(a.vc) + c * a.vc_h * kEsz + 4 * c16 * kEsz;
   const uint64_t ke_head = reinterpret_cast<uint64_t>(a.ke) + c * a.ke_h, ve_head = reinterpret_cast<uint64_t>(a.ve) + c * a.ve_h;
   const float c2 = a.scale_log2;
 
-  for (int i0 = 0; i0 < n_rows; i0 += 16) {
+  for (int i0 = rows.i0; i0 < n_rows; i0 += 16) {
     const int p_lo = uni(p_first + quot(i0, a.by_r)), p_hi = uni(p_first + quot(min(i0 + 16, n_rows) - 1, a.by_r));
     const KeyTiles kt = key_tiles<TK>(a.window, a.sinks, p_lo, p_hi, sr.keys);
     const Piece piece = pieces_of(a.few, kt.total);
@@ -452,8 +452,14 @@ __global__ void __launch_bounds__(256, 6) paged_join_kernel(PArgs a, int nq, int
   if (t >= a.T) return;
   const SeqRows sr = find_rows<-1>(a, t, tid & 63);
   if (sr.b < 0 || t < sr.s0 || t >= sr.s0 + sr.n) return;
-  const int n_rows = sr.n * a.r, p_first = sr.kv - sr.n;
-  const bool few = n_rows <= a.few_rows;
+  const int tok = t - sr.s0, p_first = sr.kv - sr.n;
+  FewRows rows{sr, 0, sr.n * a.r};                // the rows that were dealt out with it
+  const bool few = rows.i1 <= a.few_rows;
+  if (a.few_tokens > 0) {
+    const int first = quot(tok, a.by_few_tokens) * a.few_tokens;
+    rows.i0 = first * a.r;
+    rows.i1 = min(first + a.few_tokens, sr.n) * a.r;
+  }
   const int tile = few ? 16 * nq : a.chunk_rows;
   const PSet& set = few ? a.few : a.chunk;
   if (set.splits == 1) return;                    // in one piece: written by the attention kernel
@@ -463,8 +469,8 @@ __global__ void __launch_bounds__(256, 6) paged_join_kernel(PArgs a, int nq, int
   for (int hh = 0; hh < heads; hh += kGroups >> log2g) {
     const int h = h0 + hh + sub;
     const bool on = hh + sub < heads && h < H;
-    const int i = (t - sr.s0) * a.r + (h - quot(h, a.by_r) * a.r), j0 = i & ~(tile - 1);   // tile: a power of two
-    const int p_lo = p_first + quot(j0, a.by_r), p_hi = p_first + quot(min(j0 + tile, n_rows) - 1, a.by_r);
+    const int i = tok * a.r + (h - quot(h, a.by_r) * a.r), j0 = rows.i0 + ((i - rows.i0) & ~(tile - 1));   // tile: a power of two
+    const int p_lo = p_first + quot(j0, a.by_r), p_hi = p_first + quot(min(j0 + tile, rows.i1) - 1, a.by_r);
     const KeyTiles kt = few ? key_tiles<FEW_TK>(a.window, a.sinks, p_lo, p_hi, sr.keys) : key_tiles<TK>(a.window, a.sinks, p_lo, p_hi, sr.keys);
     const Piece piece = pieces_of(set, kt.total);
     const int pieces = on && piece.count > 1 ? piece.count : 0;
@@ -538,7 +544,7 @@ int join_t(const PArgs& a, int nq, hipStream_t st) {
 
 template <int D, bool E4M3>
 int launch_pages(const PArgs& a, hipStream_t st) {
-  const int few = a.B * a.Hkv * a.few.splits;
+  const int few = a.few.n_tiles * a.Hkv * a.few.splits;
   if (a.chunk_blocks == 0) return launch_blocks(paged_few_f32_kernel<D, E4M3>, few, 256, st, a);
   if (a.few_rows == 0) return launch_blocks(paged_f32_kernel<D, E4M3>, a.chunk_blocks, 256, st, a);
   return launch_blocks(paged_both_f32_kernel<D, E4M3>, a.chunk_blocks + few, 256, st, a);
