@@ -13,8 +13,10 @@ namespace s2 {
 // How the work of a launch, or of a part of it, is dealt out.
 struct PSet {
   int splits, min_tiles;                       // most pieces the keys of a row tile are cut into; fewest key tiles of one
-  int n_tiles;                                 // row tiles (chunk), sequences or tokens (few)
+  int n_tiles;                                 // row tiles (chunk), units (few)
   Div by_tiles, by_groups, by_splits, by_min;  // n_tiles, Hkv * splits, splits, min_tiles
+  float* part_o; float* part_lse;              // splits > 1: [split][part_rows][D] and [split][part_rows] (base 2)
+  long long part_rows;
 };
 
 struct PArgs {
@@ -23,7 +25,6 @@ struct PArgs {
   char* kc; char* vc;                          // cache, (pages, page_size, Hkv, D)
   uint8_t* ke; uint8_t* ve;                    // e4m3: biased exponents, (pages, page_size, Hkv)
   const int* table; const int* row_start; const int* kv_len;
-  float* part_o; float* part_lse;              // splits > 1: [split][T][H][D] and [split][T][H] (base 2)
   long long q_t, q_h, k_t, k_h, v_t, v_h;      // strides in elements
   long long kc_p, kc_t, kc_h, vc_p, vc_t, vc_h;
   long long ke_p, ke_t, ke_h, ve_p, ve_t, ve_h;
@@ -32,12 +33,23 @@ struct PArgs {
   int window, sinks;                           // window 0: every earlier key is visible
   PSet chunk, few;                             // sequences of more than few_rows (row, head of the kv head) pairs, and the others
   int few_rows, chunk_rows;                    // chunk_rows: of a row tile of `chunk`
-  int few_tokens;                              // `few` deals out so many tokens of a sequence at a time (0: a sequence's whole)
+  int few_slots;                               // rows of the pieces of `few`: few_rows of a sequence and kv head, not (T, H) (part_row)
+  int few_tokens;                              // `few` deals out so many tokens of a sequence at a time (2^30: all of them)
   int by16;                                    // pages of a multiple of 16 tokens, 16 rows of one within 31-bit offsets
   int chunk_blocks;                            // blocks of `chunk`; those of `few` follow
   Div by_r, by_page, by_Hkv, by_few_tokens;
   float scale_log2;
 };
+
+// The arguments again, as the kernels' first, for what is used only once a workgroup's keys are done: read from memory then, and not kept
+// in scalar registers (or spilled from them) until then.
+__device__ __forceinline__ PArgs late_args() {
+  auto p = (const __attribute__((address_space(4))) void*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  PArgs a;
+  __builtin_memcpy(&a, (const void*)p, sizeof(a));
+  return a;
+}
 
 __device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -61,17 +73,17 @@ __device__ __forceinline__ SeqRows seq_rows(const PArgs& a, int b) {
 // tiles of 2^SHIFT (token, query head of the kv head) pairs, of which a sequence owns those from
 // (row_start[b] * r >> SHIFT) + b on: at least as many as it needs, and no running sum is needed to place them.
 // The whole wave calls it and has one answer: up to 64 sequences are looked at together, everything about them read at once;
-// more are narrowed down by looking at every 64th part first.  Where row_start falls, the answer is some sequence.  lo, hi: only
-// sequences lo .. hi - 1 are looked at.
+// more are narrowed down by looking at every 64th part first.  Where row_start falls, the answer is some sequence.
 template <int SHIFT>
 __device__ __forceinline__ int first_tile(const PArgs& a, int s0, int b) { return (int)((unsigned)(s0 * a.r) >> SHIFT) + b; }
 template <int SHIFT>
-__device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane, int lo, int hi) {
+__device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane) {
   auto before = [&](int start, int i) __attribute__((always_inline)) {
     const int s0 = min(max(start, 0), a.T);
     if constexpr (SHIFT < 0) return s0 <= id;
     else return first_tile<SHIFT>(a, s0, i) <= id;
   };
+  int lo = 0, hi = a.B;
   while (hi - lo > 64) {
     const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
     const int m = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && before(a.row_start[min(i, hi - 1)], i)));
@@ -89,34 +101,38 @@ __device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane, i
   s.keys = min(s.kv, a.max_keys);
   return s;
 }
-template <int SHIFT>
-__device__ __forceinline__ SeqRows find_rows(const PArgs& a, int id, int lane) { return find_rows<SHIFT>(a, id, lane, 0, a.B); }
 
 // Rows i0 .. i1 - 1 of a sequence's (token, query head of the kv head) pairs: those of a workgroup of `few`, by turns where it holds fewer.
 struct FewRows {
   SeqRows sr;
   int i0, i1;
 };
-// The rows of unit u: a sequence of up to few_rows rows, or, from the u-th token on, the next few_tokens ones of its sequence.  The latter
-// where there are no more tokens than sequences, as in a step of single tokens: unit u is then of sequence u or, where some have no row,
-// of one of the next, which are looked at first.  A sequence that has several tokens after all has workgroups for all of them.
+// The rows of unit u < B: those of the first few_tokens tokens of sequence u, if they are few_rows or less.  Its other tokens, which a
+// step of single tokens does not have, are units behind those: unit B + j - 1 has the few_tokens ones that begin in the j-th few_tokens
+// rows of the call (one stretch of a sequence but its first does, at most).
+template <bool BOTH>   // beside `chunk`: u < B, and all tokens
 __device__ __forceinline__ bool few_rows_of(const PArgs& a, int u, int lane, FewRows& x) {
-  if (a.few_tokens == 0) {
-    if (u >= a.B) return false;
+  if (u >= a.few.n_tiles) return false;
+  int tok = 0;
+  if (BOTH || u < a.B) {
     x.sr = seq_rows(a, u);
-    x.i0 = 0;
-    x.i1 = wave_uniform(x.sr.n * a.r);
-    return x.i1 <= a.few_rows;
+  } else {
+    const int t0 = (u - a.B + 1) * a.few_tokens, t1 = min(t0 + a.few_tokens, a.T) - 1;
+    for (int t = t0;; t = t1) {   // the sequences of the first and of the last of them
+      x.sr = find_rows<-1>(a, t, lane);
+      tok = x.sr.b < 0 ? 0 : quot(max(min(t1 - x.sr.s0, x.sr.n - 1), 0), a.by_few_tokens) * a.few_tokens;
+      if (tok > 0 && x.sr.s0 + tok >= t0) break;
+      if (t == t1) return false;
+    }
   }
-  if (u >= a.T) return false;
-  const int near = min(u + 64, a.B);   // (u is less than B too)
-  x.sr = find_rows<-1>(a, u, lane, u, near);
-  if (x.sr.b < 0 || (x.sr.b == near - 1 && near < a.B)) x.sr = find_rows<-1>(a, u, lane);
-  const int tok = u - x.sr.s0, part = quot(max(tok, 0), a.by_few_tokens);
-  if (x.sr.b < 0 || tok < 0 || tok >= x.sr.n || tok != part * a.few_tokens) return false;
   x.i0 = wave_uniform(tok * a.r);
-  x.i1 = wave_uniform(min(tok + a.few_tokens, x.sr.n) * a.r);
-  return true;
+  x.i1 = wave_uniform((BOTH ? x.sr.n : min(tok + a.few_tokens, x.sr.n)) * a.r);
+  return x.i1 <= a.few_rows;
+}
+
+// Row of a piece for query head h of token t, the i-th of its sequence's and kv head's rows.
+__device__ __forceinline__ size_t part_row(const PArgs& a, const PSet& set, bool slots, int split, int b, int c, int i, int t, int h) {
+  return (size_t)split * set.part_rows + (slots ? ((size_t)b * a.few_rows + i) * a.Hkv + c : (size_t)t * (a.Hkv * a.r) + h);
 }
 
 // Block -> (row tile, kv head, split).  Blocks of one (kv head, split) read the same keys: whole such groups go to an XCD

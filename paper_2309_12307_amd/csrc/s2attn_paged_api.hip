@@ -70,7 +70,7 @@ struct Plan {
   bool chunk, few;
   int chunk_rows;              // of a row tile of `chunk`
   int nq, few_rows;            // 16-row blocks of a `few` workgroup; the most rows of a sequence that goes there
-  int few_tokens;              // tokens dealt out at a time there, 0: sequences
+  int few_tokens;              // tokens of a sequence dealt out at a time there
   int chunk_splits, chunk_min; // pieces, key tiles of a piece at least
   int few_splits, few_min;
 };
@@ -79,7 +79,7 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   const long long r = p->H / p->Hkv, rows = p->T * r, seqs = std::max(1, std::min(p->B, p->T));
   // One token a sequence (as far as T and B tell), of up to 16 rows (e4m3 32 in two blocks, fp32 64 in turns): all go to `few`, by as many
   // tokens as a turn takes: a sequence that has several after all, among empty slots, has workgroups for all of them (256 rows of one
-  // of 256 sequences over 8192 keys, H = 64, Hkv = 8, D = 128: 0.93 ms; by turns of one workgroup to a kv head 16.0; as the only
+  // of 256 sequences over 8192 keys, H = 64, Hkv = 8, D = 128: 0.60 ms; by turns of one workgroup to a kv head 16.0; as the only
   // sequence, in `chunk`, 0.09).  Rows that are few in all go there by turns.  Where some sequences have more, those of up to 16 rows (fp32 64) go there and the others to `chunk`.  us, all
   // in `chunk` and all in `few`, 4000 keys, D = 128: fp32, one sequence of 16 rows 35.8 and 19.9, of 64 65.9 and 57.2, eight of 16 78 and
   // 56; bf16, one of 16 15.2 and 14.6, of 24 15.6 and 15.9, eight of 20 30.5 and 43.6; e4m3, one of 24 20.4 and 15.4, eight of 20 32 and
@@ -87,6 +87,7 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   const bool f32 = p->dtype == S2ATTN_F32, e4m3 = p->cache_dtype == S2ATTN_E4M3;
   const long long most_few = f32 ? 64 : e4m3 ? 32 : 16;
   x.nq = 1;
+  x.few_tokens = (int)kMost;
   if ((p->T <= p->B && r <= most_few) || rows <= most_few) {
     x.few = true;
     if (!f32 && (p->T <= p->B ? r : rows) > 16) x.nq = 2;
@@ -94,8 +95,9 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
     if (p->T <= p->B) x.few_tokens = std::max(1, 16 * x.nq / (int)r);
   } else {
     x.chunk = true;
-    x.few = p->B > 1;
-    x.few_rows = !x.few ? 0 : f32 ? 64 : 16;
+    x.few_rows = f32 ? 64 : 16;
+    x.few = p->B > 1 && r <= x.few_rows;   // (else one token is more)
+    if (!x.few) x.few_rows = 0;
   }
   const long long most = (long long)p->table_cols * p->page_size;
   long long keys = p->max_kv > 0 ? std::min<long long>(p->max_kv, most) : most;
@@ -124,7 +126,30 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   return x;
 }
 
-size_t piece_bytes(const s2attn_paged_params* p) { return (size_t)p->T * p->H * (p->D + 1) * sizeof(float); }
+// Where the pieces' outputs go.  A piece of the rows of the call has room for all of them, (T, H) rows; sequences of few rows that are in
+// more pieces than the others have slots of their own instead, few_rows a sequence and kv head, where that is less:
+// the others may be prompts of any length.
+struct Room {
+  bool slots;
+  size_t piece, slot_piece;    // bytes of a piece
+  size_t wanted;
+};
+Room room(const s2attn_paged_params* p, const Plan& x) {
+  Room y{};
+  const size_t row = (p->D + 1) * sizeof(float);
+  y.piece = (size_t)p->T * p->H * row;
+  const int most = std::max(x.chunk_splits, x.few_splits);
+  y.wanted = most > 1 ? most * y.piece : 0;
+  if (x.chunk && x.few_splits > 1) {
+    y.slot_piece = (size_t)p->B * x.few_rows * p->Hkv * row;
+    size_t apart = x.few_splits * y.slot_piece;
+    // beside pieces of all rows in whole ones, so that workspace_bytes / piece is the number that a workspace holds
+    if (x.chunk_splits > 1) apart = (x.chunk_splits + (apart + y.piece - 1) / y.piece) * y.piece;
+    y.slots = apart < y.wanted;
+    if (y.slots) y.wanted = apart;
+  }
+  return y;
+}
 
 int check(const s2attn_paged_params* p, int call) {
   if (!p) return S2ATTN_ERR_NULL;
@@ -221,9 +246,7 @@ int s2attn_check_paged_args(const s2attn_paged_params* p, int call) { return che
 
 size_t s2attn_paged_workspace_bytes(const s2attn_paged_params* p) {
   if (!p || !shape_valid(p) || p->H % p->Hkv != 0) return 0;
-  const Plan x = plan(p, make_args(p, p->H).by16);
-  const int splits = std::max(x.chunk_splits, x.few_splits);
-  return splits > 1 ? splits * piece_bytes(p) : 0;
+  return room(p, plan(p, make_args(p, p->H).by16)).wanted;
 }
 
 int s2attn_cache_write(const s2attn_paged_params* p, void* stream) {
@@ -246,8 +269,19 @@ int s2attn_paged_fwd(const s2attn_paged_params* p, void* stream) {
   if (rc != S2ATTN_OK || p->T == 0) return rc;
   s2::PArgs a = make_args(p, p->H);
   const Plan x = plan(p, a.by16);
-  const long long fit = p->workspace ? (long long)(p->workspace_bytes / piece_bytes(p)) : 0;
-  auto set = [&](s2::PSet& s, int n_tiles, int splits, int min_tiles) {
+  // the pieces that the workspace holds: in one area, or slots, which get what the others leave but half of it at least, and the others
+  const Room y = room(p, x);
+  const size_t bytes = p->workspace ? p->workspace_bytes : 0;
+  char* ws = static_cast<char*>(p->workspace);
+  size_t few_bytes = 0;
+  long long fit_chunk = bytes / y.piece, fit_few = fit_chunk;
+  if (y.slots) {
+    const size_t others = x.chunk_splits > 1 ? x.chunk_splits * y.piece : 0;
+    fit_few = std::min<long long>(x.few_splits, std::max(bytes / 2, bytes - std::min(bytes, others)) / y.slot_piece);
+    if (fit_few > 1) few_bytes = fit_few * y.slot_piece;
+    fit_chunk = (bytes - few_bytes) / y.piece;
+  }
+  auto set = [&](s2::PSet& s, int n_tiles, int splits, int min_tiles, long long fit, char* part, size_t piece) {
     const long long grid = (kMost / 2) / std::max(1LL, (long long)n_tiles * p->Hkv);
     s.splits = (int)std::max<long long>(1, std::min<long long>(splits, std::min(fit, grid)));
     s.min_tiles = min_tiles;
@@ -256,20 +290,21 @@ int s2attn_paged_fwd(const s2attn_paged_params* p, void* stream) {
     s.by_groups = s2::div_by(p->Hkv * s.splits);
     s.by_splits = s2::div_by(s.splits);
     s.by_min = s2::div_by(min_tiles);
+    s.part_rows = piece / ((p->D + 1) * sizeof(float));
+    s.part_o = reinterpret_cast<float*>(part);
     return n_tiles * p->Hkv * s.splits;
   };
   a.few_rows = x.few_rows;
   a.few_tokens = x.few_tokens;
-  a.by_few_tokens = s2::div_by(std::max(1, x.few_tokens));
+  a.by_few_tokens = s2::div_by(x.few_tokens);
   a.chunk_rows = x.chunk_rows;
-  a.chunk_blocks = set(a.chunk, (int)row_tiles(p, x.chunk_rows), x.chunk_splits, x.chunk_min);
+  a.chunk_blocks = set(a.chunk, (int)row_tiles(p, x.chunk_rows), x.chunk_splits, x.chunk_min, fit_chunk, ws + few_bytes, y.piece);
   if (!x.chunk) a.chunk_blocks = 0;
-  set(a.few, x.few_tokens > 0 ? p->T : p->B, x.few_splits, x.few_min);
+  a.few_slots = y.slots;
+  set(a.few, p->B + (p->T - 1) / x.few_tokens, x.few_splits, x.few_min, fit_few, ws, y.slots ? y.slot_piece : y.piece);
   const int splits = std::max(a.chunk.splits, a.few.splits);
-  if (splits > 1) {
-    a.part_o = static_cast<float*>(p->workspace);
-    a.part_lse = a.part_o + (size_t)splits * p->T * p->H * p->D;
-  }
+  for (s2::PSet* s : {&a.chunk, &a.few})
+    s->part_lse = s->part_o + (size_t)(y.slots ? s->splits : splits) * s->part_rows * p->D;   // behind all pieces of the area
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf16 = p->dtype == S2ATTN_BF16, e4m3 = p->cache_dtype == S2ATTN_E4M3;
   rc = bf16 ? s2::launch_paged_bf16(a, p->D, e4m3, x.nq, st) : s2::launch_paged_f32(a, p->D, e4m3, st);

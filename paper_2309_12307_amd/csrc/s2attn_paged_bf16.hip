@@ -7,9 +7,10 @@
 //          tensors.  Bound by the matrix unit (2048 rows over 32768 keys, H = 32, D = 128: 990 us, 1080 TFLOP/s; D = 64 by the vector
 //          unit, which has twice the exponentials for a product).
 //   few    all rows of a sequence that has up to 16 (e4m3: 32), as single tokens have, or as many of its tokens as make that, and a
-//          piece of its keys; the waves take different 32-key tiles and meet once, at the end.  Bound by HBM: what counts is bytes on the way, so a wave has a whole tile of
-//          K and V on its way to registers while it works on another, and waits for nobody (two sequences over 100 000 tokens,
-//          e4m3, 32 kv heads: 290 us, 5.7 TB/s; 32 over up to 8192, bf16, 8 kv heads: 86 us and the join 5).
+//          piece of its keys; the waves take different 32-key tiles and meet once, at the end.  Bound by HBM: what counts is bytes
+//          on the way, so a wave has a whole tile of K and V on its way to registers while it works on another, and waits for
+//          nobody (two sequences over 100 000 tokens, e4m3, 32 kv heads: 290 us, 5.7 TB/s; 32 over up to 8192, bf16, 8 kv heads: 86
+//          us and the join 5).
 // Rows that several pieces share leave normalised fp32 partial outputs and their log-sum-exp, which a second kernel joins.
 //
 // P is rounded to bf16 for the second product (as everywhere in this library); the row sum adds the unrounded P, and
@@ -46,10 +47,11 @@ __device__ __forceinline__ void mask_paged(f32x16& s0, f32x16& s1, int key0, int
 // A wave's 32 rows from iw on (lane l and l + 32: row l, token t and head h): o / l and the log-sum-exp, as a piece or as the
 // output, the latter turned through the wave's part of LDS.  A row that saw nothing: 0 and -infinity.  m2: maximum, base 2.
 template <int D>
-__device__ __forceinline__ void chunk_epilogue(const PArgs& a, const f32x16 (&o)[D / 32], float m2, float l_run, char* region, int s0, int c,
+__device__ __forceinline__ void chunk_epilogue(const f32x16 (&o)[D / 32], float m2, float l_run, char* region, int s0, int c,
                                                int iw, int n_rows, int t, int h, int split, int pieces, int lane) {
   using L = Tile<D>;
   constexpr int DB = D / 32, kChunks = D / 8, kRowsPer = 64 / kChunks;
+  const PArgs a = late_args();
   const int g32 = lane >> 5, l32 = lane & 31;
   const float l_tot = sum_halves(l_run);
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
@@ -58,15 +60,15 @@ __device__ __forceinline__ void chunk_epilogue(const PArgs& a, const f32x16 (&o)
   const int H = a.Hkv * a.r;
   if (pieces > 1) {
     if (!valid) return;
-    const size_t at = ((size_t)split * a.T + t) * H + h;
-    float* dst = a.part_o + at * D + 4 * g32;
+    const size_t at = part_row(a, a.chunk, false, split, 0, c, 0, t, h);
+    float* dst = a.chunk.part_o + at * D + 4 * g32;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int vv = 0; vv < 4; ++vv)
         *reinterpret_cast<float4*>(dst + 32 * db + 8 * vv) =
             make_float4(o[db][4 * vv] * inv, o[db][4 * vv + 1] * inv, o[db][4 * vv + 2] * inv, o[db][4 * vv + 3] * inv);
-    if (g32 == 0) a.part_lse[at] = lse2;
+    if (g32 == 0) a.chunk.part_lse[at] = lse2;
     return;
   }
 #pragma unroll
@@ -336,7 +338,7 @@ __device__ __forceinline__ void chunk_workgroup(const PArgs& a, int block, char*
   __syncthreads();
 
   if (idle) return;
-  chunk_epilogue<D>(a, o, m_run * c2, l_run, smem + w * 32 * L::kRow, sr.s0, c, iw, n_rows, t, h, split, piece.count, lane);
+  chunk_epilogue<D>(o, m_run * c2, l_run, smem + w * 32 * L::kRow, sr.s0, c, iw, n_rows, t, h, split, piece.count, lane);
 }
 
 // The same for 256 rows: eight waves and three stages, the walk of the eight-wave forward (D = 128, pages of a multiple of 16).
@@ -461,7 +463,7 @@ __global__ void __launch_bounds__(512, 1) paged_long_kernel(PArgs a, int first_b
           });
   __syncthreads();
   if (idle) return;
-  chunk_epilogue<D>(a, st.o_acc, st.m_run * c2, st.l_run, smem + w * 32 * kRowBytes, sr.s0, c, iw, n_rows, t, h, split, piece.count, lane);
+  chunk_epilogue<D>(st.o_acc, st.m_run * c2, st.l_run, smem + w * 32 * kRowBytes, sr.s0, c, iw, n_rows, t, h, split, piece.count, lane);
 }
 
 // ---- few rows.  v_mfma_f32_16x16x32_bf16, lane l: c16 = l % 16, q4 = l / 16 (operand layout: s2attn_bf16_common.h).
@@ -477,7 +479,8 @@ struct FewTile {
   uint32_t seen;                                   // a bit for each key that exists and that some row sees
 };
 
-template <int D, bool E4M3, bool BY16, int NQ>
+// BOTH: beside the other kind of workgroup
+template <int D, bool E4M3, bool BY16, int NQ, bool BOTH>
 __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* smem) {
   using T = FewTile<D, E4M3>;
   constexpr int TK = 32, kWaves = 4, kRow = D * 2, KF = D / 32, DB = D / 16;   // KF: operands of a key over D
@@ -487,7 +490,7 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
   const int y = quot(block, a.by_Hkv), c = block - y * a.Hkv;
   const int unit = quot(y, a.few.by_splits), split = y - unit * a.few.splits;
   FewRows rows;
-  if (!few_rows_of(a, unit, lane, rows)) return;
+  if (!few_rows_of<BOTH>(a, unit, lane, rows)) return;
   const SeqRows sr = rows.sr;
   const int b = sr.b, n_rows = rows.i1, p_first = uni(sr.kv - sr.n);
 
@@ -705,6 +708,7 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
     }
 
     // ---- the waves' sums meet
+    const PArgs z = BOTH ? late_args() : a;
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) l_run[qb] = sum_of_4(l_run[qb]);
     __syncthreads();   // every wave is done with its V
@@ -738,16 +742,16 @@ __device__ __forceinline__ void few_workgroup(const PArgs& a, int block, char* s
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const float lse2 = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
-      const int tq = quot(i0 + row, a.by_r), h = c * a.r + i0 + row - tq * a.r, t = sr.s0 + tq, H = a.Hkv * a.r;
+      const int tq = quot(i0 + row, z.by_r), h = c * z.r + i0 + row - tq * z.r, t = sr.s0 + tq, H = z.Hkv * z.r;
       if (piece.count > 1) {
-        const size_t dst = ((size_t)split * a.T + t) * H + h;
-        f32x4* po = reinterpret_cast<f32x4*>(a.part_o + dst * D + 8 * ch);
+        const size_t dst = part_row(z, z.few, z.few_slots, split, b, c, i0 + row, t, h);
+        f32x4* po = reinterpret_cast<f32x4*>(z.few.part_o + dst * D + 8 * ch);
         po[0] = s0 * inv;
         po[1] = s1 * inv;
-        if (ch == 0) a.part_lse[dst] = lse2;
+        if (ch == 0) z.few.part_lse[dst] = lse2;
       } else {
-        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(a.o) + ((size_t)t * H + h) * D + 8 * ch) = pack8(s0 * inv, s1 * inv);
-        if (ch == 0 && a.lse) a.lse[(size_t)h * a.T + t] = lse2 * kLn2;
+        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(z.o) + ((size_t)t * H + h) * D + 8 * ch) = pack8(s0 * inv, s1 * inv);
+        if (ch == 0 && z.lse) z.lse[(size_t)h * z.T + t] = lse2 * kLn2;
       }
     }
     if constexpr (NQ > 1) return;   // 32 rows at most: no other turn
@@ -770,7 +774,7 @@ __global__ void __launch_bounds__(256, 2) paged_chunk_kernel(PArgs a, int first_
 template <int D, bool E4M3, bool BY16, int NQ>
 __global__ void __launch_bounds__(256, 2) paged_few_kernel(PArgs a, int first_block) {
   __shared__ __attribute__((aligned(1024))) char smem[kFewBytes<D, NQ>];
-  few_workgroup<D, E4M3, BY16, NQ>(a, first_block + block_id(), smem);
+  few_workgroup<D, E4M3, BY16, NQ, false>(a, first_block + block_id(), smem);
 }
 
 template <int D, bool E4M3, bool BY16>
@@ -781,7 +785,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_both_kernel(PArgs 
   if (block < a.chunk_blocks)   // the long chains first: 62 us, the others first 72 (16 sequences of 1 to 600 rows, window 4096)
     chunk_workgroup<D, E4M3, BY16>(a, block, smem, flags);
   else
-    few_workgroup<D, E4M3, BY16, 1>(a, block - a.chunk_blocks, smem);
+    few_workgroup<D, E4M3, BY16, 1, true>(a, block - a.chunk_blocks, smem);
 }
 
 template <int D, bool E4M3, bool BY16>

@@ -197,15 +197,16 @@ __device__ __forceinline__ void chunk_f32_workgroup(const PArgs& a, int block, c
   if (iw + c16 >= n_rows) return;
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
   const float lse2 = l_tot == 0.f ? -INFINITY : m_run + log2f(l_tot);
-  const int H = a.Hkv * a.r;
+  const PArgs z = late_args();
+  const int H = z.Hkv * z.r;
   if (piece.count > 1) {
-    const size_t at = ((size_t)split * a.T + t) * H + h;
-    store_row<D>(a.part_o + at * D, o, inv, q4);
-    if (q4 == 0) a.part_lse[at] = lse2;
+    const size_t at = part_row(z, z.chunk, false, split, b, c, 0, t, h);
+    store_row<D>(z.chunk.part_o + at * D, o, inv, q4);
+    if (q4 == 0) z.chunk.part_lse[at] = lse2;
     return;
   }
-  store_row<D>(static_cast<float*>(a.o) + ((size_t)t * H + h) * D, o, inv, q4);
-  if (q4 == 0 && a.lse) a.lse[(size_t)h * a.T + t] = lse2 * kLn2;
+  store_row<D>(static_cast<float*>(z.o) + ((size_t)t * H + h) * D, o, inv, q4);
+  if (q4 == 0 && z.lse) z.lse[(size_t)h * z.T + t] = lse2 * kLn2;
 }
 
 // ---- few rows: sixteen rows of a sequence at a time, the waves on different tiles of 16 keys, K and V straight to registers, the next
@@ -221,7 +222,7 @@ struct FewTile {
   uint32_t seen;
 };
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool BOTH>   // BOTH: beside the other kind of workgroup
 __device__ __forceinline__ void few_f32_workgroup(const PArgs& a, int block, float* blocks, float (*max_s)[16], float (*sum_s)[16]) {
   using T = FewTile<D, E4M3>;
   constexpr int TK = 16, kWaves = 4, kEsz = E4M3 ? 1 : 4, kStride = D + 4;
@@ -230,7 +231,7 @@ __device__ __forceinline__ void few_f32_workgroup(const PArgs& a, int block, flo
   const int y = quot(block, a.by_Hkv), c = block - y * a.Hkv;
   const int unit = quot(y, a.few.by_splits), split = y - unit * a.few.splits;
   FewRows rows;
-  if (!few_rows_of(a, unit, lane, rows)) return;
+  if (!few_rows_of<BOTH>(a, unit, lane, rows)) return;
   const SeqRows sr = rows.sr;
   const int b = sr.b, n_rows = rows.i1, p_first = uni(sr.kv - sr.n);
   const uint64_t k_head = reinterpret_cast<uint64_t>(a.kc) + c * a.kc_h * kEsz + 16 * q4;
@@ -363,6 +364,7 @@ __device__ __forceinline__ void few_f32_workgroup(const PArgs& a, int block, flo
       if (n + kWaves < n1) step(tb, ta, n + kWaves);
     }
 
+    const PArgs z = BOTH ? late_args() : a;
     l_run = sum_cols(l_run);
 #pragma unroll
     for (int j = 0; j < D / 64; ++j)
@@ -391,15 +393,15 @@ __device__ __forceinline__ void few_f32_workgroup(const PArgs& a, int block, flo
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-      const int ti = quot(i0 + r16, a.by_r), hi = c * a.r + i0 + r16 - ti * a.r, tt = sr.s0 + ti, H = a.Hkv * a.r;
+      const int ti = quot(i0 + r16, z.by_r), hi = c * z.r + i0 + r16 - ti * z.r, tt = sr.s0 + ti, H = z.Hkv * z.r;
       float* dst;
       if (piece.count > 1) {
-        const size_t at2 = ((size_t)split * a.T + tt) * H + hi;
-        dst = a.part_o + at2 * D;
-        if (ch == 0) a.part_lse[at2] = lse2;
+        const size_t at2 = part_row(z, z.few, z.few_slots, split, b, c, i0 + r16, tt, hi);
+        dst = z.few.part_o + at2 * D;
+        if (ch == 0) z.few.part_lse[at2] = lse2;
       } else {
-        dst = static_cast<float*>(a.o) + ((size_t)tt * H + hi) * D;
-        if (ch == 0 && a.lse) a.lse[(size_t)hi * a.T + tt] = lse2 * kLn2;
+        dst = static_cast<float*>(z.o) + ((size_t)tt * H + hi) * D;
+        if (ch == 0 && z.lse) z.lse[(size_t)hi * z.T + tt] = lse2 * kLn2;
       }
       *reinterpret_cast<f32x4*>(dst + 8 * ch) = s0 * inv;
       *reinterpret_cast<f32x4*>(dst + 8 * ch + 4) = s1 * inv;
@@ -423,7 +425,7 @@ template <int D, bool E4M3>
 __global__ void __launch_bounds__(256, 2) paged_few_f32_kernel(PArgs a, int first_block) {
   __shared__ __attribute__((aligned(16))) float blocks[kFewBytes<D> / 4];
   __shared__ float max_s[4][16], sum_s[4][16];
-  few_f32_workgroup<D, E4M3>(a, first_block + block_id(), blocks, max_s, sum_s);
+  few_f32_workgroup<D, E4M3, false>(a, first_block + block_id(), blocks, max_s, sum_s);
 }
 
 template <int D, bool E4M3>
@@ -435,47 +437,55 @@ __global__ void __launch_bounds__(256, 2) paged_both_f32_kernel(PArgs a, int fir
   if (block < a.chunk_blocks)
     chunk_f32_workgroup<D, E4M3>(a, block, smem);
   else
-    few_f32_workgroup<D, E4M3>(a, block - a.chunk_blocks, reinterpret_cast<float*>(smem), max_s, sum_s);
+    few_f32_workgroup<D, E4M3, true>(a, block - a.chunk_blocks, reinterpret_cast<float*>(smem), max_s, sum_s);
 }
 
 // o = sum of the pieces' outputs by their share exp2(lse_s - lse) of the row.  D / 4 lanes hold a piece's output; G groups of so
 // many lanes take the pieces of one row, four at a time (each group with a running maximum of its own), the other groups of a
 // workgroup other heads of the same token, `heads` of them to a workgroup.  Bound by latency: six workgroups to a CU hide it
 // better than the four that the compiler would have left room for (13.4 and 11.2 us for the case below).
-template <int D, int TK, int FEW_TK, bool BF16>
-__global__ void __launch_bounds__(256, 6) paged_join_kernel(PArgs a, int nq, int heads, int head_blocks, Div by_head_blocks, int first_block) {
+// FEW: only sequences of `few` are in pieces, in slots, and of each only the first per_seq tokens are looked at.
+template <int D, int TK, int FEW_TK, bool BF16, bool FEW>
+__global__ void __launch_bounds__(256, 6) paged_join_kernel(PArgs a, int nq, int heads, int head_blocks, Div by_head_blocks, int per_seq,
+                                                            Div by_seq, int first_block) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
   __shared__ float4 acc_s[kGroups][kLanes];
   __shared__ float m_s[kGroups], l_s[kGroups];
   const int tid = thread_id(), H = a.Hkv * a.r;
-  const int block = first_block + block_id(), t = quot(block, by_head_blocks), h0 = (block - t * head_blocks) * heads;
-  if (t >= a.T) return;
-  const SeqRows sr = find_rows<-1>(a, t, tid & 63);
-  if (sr.b < 0 || t < sr.s0 || t >= sr.s0 + sr.n) return;
-  const int tok = t - sr.s0, p_first = sr.kv - sr.n;
-  FewRows rows{sr, 0, sr.n * a.r};                // the rows that were dealt out with it
-  const bool few = rows.i1 <= a.few_rows;
-  if (a.few_tokens > 0) {
-    const int first = quot(tok, a.by_few_tokens) * a.few_tokens;
-    rows.i0 = first * a.r;
-    rows.i1 = min(first + a.few_tokens, sr.n) * a.r;
+  const int block = first_block + block_id(), unit = quot(block, by_head_blocks), h0 = (block - unit * head_blocks) * heads;
+  int t = unit;
+  SeqRows sr;
+  if constexpr (FEW) {
+    const int b = quot(unit, by_seq);
+    if (b >= a.B) return;
+    sr = seq_rows(a, b);
+    t = sr.s0 + unit - b * per_seq;
+  } else {
+    if (t >= a.T) return;
+    sr = find_rows<-1>(a, t, tid & 63);
   }
+  if (sr.b < 0 || t < sr.s0 || t >= sr.s0 + sr.n) return;
+  const int tok = t - sr.s0, p_first = sr.kv - sr.n, first = quot(tok, a.by_few_tokens) * a.few_tokens;
+  const bool few = sr.n * a.r <= a.few_rows;
+  if (FEW && !few) return;
+  const int i0 = first * a.r, i1 = min(first + a.few_tokens, sr.n) * a.r;   // the rows that were dealt out with it
   const int tile = few ? 16 * nq : a.chunk_rows;
   const PSet& set = few ? a.few : a.chunk;
   if (set.splits == 1) return;                    // in one piece: written by the attention kernel
   const int log2g = set.splits <= 4 ? 0 : set.splits <= 8 ? 1 : set.splits <= 16 ? 2 : 3;
   const int g = tid / kLanes, l = tid % kLanes, sub = g >> log2g, piece0 = g & ((1 << log2g) - 1);
-  const size_t step = (size_t)a.T * H;
+  const size_t step = set.part_rows;
   for (int hh = 0; hh < heads; hh += kGroups >> log2g) {
     const int h = h0 + hh + sub;
     const bool on = hh + sub < heads && h < H;
-    const int i = tok * a.r + (h - quot(h, a.by_r) * a.r), j0 = rows.i0 + ((i - rows.i0) & ~(tile - 1));   // tile: a power of two
-    const int p_lo = p_first + quot(j0, a.by_r), p_hi = p_first + quot(min(j0 + tile, rows.i1) - 1, a.by_r);
+    const int i = tok * a.r + (h - quot(h, a.by_r) * a.r), j0 = i0 + ((i - i0) & ~(tile - 1));   // tile: a power of two
+    const int p_lo = p_first + quot(j0, a.by_r), p_hi = p_first + quot(min(j0 + tile, i1) - 1, a.by_r);
     const KeyTiles kt = few ? key_tiles<FEW_TK>(a.window, a.sinks, p_lo, p_hi, sr.keys) : key_tiles<TK>(a.window, a.sinks, p_lo, p_hi, sr.keys);
     const Piece piece = pieces_of(set, kt.total);
     const int pieces = on && piece.count > 1 ? piece.count : 0;
-    const float* po = a.part_o + ((size_t)t * H + h) * D + 4 * l;
-    const float* pl = a.part_lse + (size_t)t * H + h;
+    const size_t row = part_row(a, set, FEW || (few && a.few_slots), 0, sr.b, quot(h, a.by_r), i, t, h);
+    const float* po = set.part_o + row * D + 4 * l;
+    const float* pl = set.part_lse + row;
     float m = -FLT_MAX, sum = 0.f;
     float4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = piece0; s0 < pieces; s0 += 4 << log2g) {
@@ -534,12 +544,16 @@ template <int D, int TK, int FEW_TK, bool BF16>
 int join_t(const PArgs& a, int nq, hipStream_t st) {
   constexpr int kGroups = 1024 / D;
   const int H = a.Hkv * a.r, splits = a.few.splits > a.chunk.splits ? a.few.splits : a.chunk.splits;
+  const int per_seq = a.few_slots && a.chunk.splits == 1 ? a.few_rows / a.r : 0, units = per_seq > 0 ? a.B * per_seq : a.T;
   // heads go together while 2048 workgroups are left: 16 sequences of 1 to 600 rows, H = 32, D = 64, down to 512, 2048 and 4096
   // 20, 10.0 and 11.2 us
   int heads = splits <= 4 ? kGroups : splits <= 8 ? kGroups / 2 : splits <= 16 ? kGroups / 4 : kGroups / 8;
-  while (2 * heads <= H && (long long)a.T * (H / (2 * heads)) >= 2048) heads *= 2;
+  while (2 * heads <= H && (long long)units * (H / (2 * heads)) >= 2048) heads *= 2;
   const int head_blocks = (H + heads - 1) / heads;
-  return launch_blocks(paged_join_kernel<D, TK, FEW_TK, BF16>, a.T * head_blocks, 256, st, a, nq, heads, head_blocks, div_by(head_blocks));
+  auto launch = [&](auto kernel) {
+    return launch_blocks(kernel, units * head_blocks, 256, st, a, nq, heads, head_blocks, div_by(head_blocks), per_seq, div_by(per_seq > 0 ? per_seq : 1));
+  };
+  return per_seq > 0 ? launch(paged_join_kernel<D, TK, FEW_TK, BF16, true>) : launch(paged_join_kernel<D, TK, FEW_TK, BF16, false>);
 }
 
 template <int D, bool E4M3>
