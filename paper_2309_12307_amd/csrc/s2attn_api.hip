@@ -237,7 +237,7 @@ bool dq_reuses_input(const s2attn_params* p) {
 // ---- window attention: one causal run of all tokens, no groups or shifts.
 struct WindowPlan {
   bool small_fwd, small_bwd;   // the kernels for few rows
-  int parts;
+  int parts, cut_keys;         // cut_keys: keys of the cut key tiles
   s2::Win win;
   size_t rows, partial, far;   // bytes of the workspace: row terms, partial dk, dv of the parts, of the cut key tiles
 };
@@ -282,6 +282,7 @@ WindowPlan window_plan(const s2attn_params* p, int window, int sinks, size_t ava
   const int main_tiles = std::min<long long>(all, (KT - 1LL + x.win.window + QT - 1) / QT);
   if (tiles > 0 && tiles <= kMostCutTiles && all > main_tiles) {
     x.win.sink_tiles = tiles;
+    x.cut_keys = tiles * KT;
     const long long seqs = (long long)p->B * p->Hkv, work = seqs * ((p->N + KT - 1) / KT) * main_tiles + seqs * tiles * (all - main_tiles);
     x.win.seg_tiles = std::max(std::max(std::min(main_tiles, 6), (main_tiles + 2) / 3), (all - main_tiles + kMostSegments - 1) / kMostSegments);
     x.win.seg_tiles = (int)std::min<long long>(std::max<long long>(x.win.seg_tiles, work / 256 / 32), all - main_tiles);
@@ -612,8 +613,8 @@ int s2attn_window_bwd(const s2attn_params* p, int window, int sinks, void* strea
     rc = s2::launch_delta_bf16(a, st);
     if (rc == 0) rc = s2::launch_window_bwd_bf16(a, x.win, dq_last, st);
   }
-  // (the parts' sum leaves cut key tiles to the sum of their segments, which comes after it)
-  if (rc == 0 && a.parts > 1) rc = s2::launch_combine_partials(a, p->dtype, st);
+  // the parts of cut key tiles lie with their segments, and are summed with them
+  if (rc == 0 && a.parts > 1) rc = s2::launch_combine_partials(a, p->dtype, st, x.cut_keys);
   if (rc == 0 && x.win.sink_tiles > 0) rc = s2::launch_sink_combine(a, x.win, p->dtype, x.small_bwd, st);
   return rc == 0 ? S2ATTN_OK : S2ATTN_ERR_LAUNCH;
 }

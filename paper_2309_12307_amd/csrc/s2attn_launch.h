@@ -34,8 +34,8 @@ int launch_bwd_dq_spill_bf16(const KArgs& a, hipStream_t st);
 
 // delta[b,h,t] = sum_d dout[b,t,h,d] * o[b,t,h,d], fp32, and lse2
 int launch_delta_bf16(const KArgs& a, hipStream_t st);
-// dk = sum of the partials of all parts (same for dv), cast to the output type
-int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st);
+// dk = sum of the partials of all parts (same for dv), cast to the output type; keys before first_key are left as they are
+int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st, int first_key = 0);
 
 // Window attention: forward; dK/dV and dQ (bf16: delta must be ready), dk, dv of cut key tiles left as partials; their sum
 int launch_window_fwd_f32(const KArgs& a, Win win, hipStream_t st);

@@ -75,10 +75,10 @@ __global__ void __launch_bounds__(256) delta_kernel(const void* o, const void* d
   }
 }
 
-// dk (dv) = sum of the `parts` contiguous fp32 partials, in order.
+// dk (dv) = sum of the `parts` contiguous fp32 partials, in order, of the keys from first_key on.
 template <bool BF16>
 __global__ void __launch_bounds__(256) combine_kernel(const float* partial, void* dk, void* dv, TStride sdk,
-                                                      TStride sdv, int N, int Hkv, int D, int parts, size_t elems) {
+                                                      TStride sdv, int N, int Hkv, int D, int parts, size_t elems, int first_key) {
   const size_t i4 = ((size_t)block_id() * 256 + thread_id()) * 4;
   if (i4 >= elems) return;
   // contiguous (b, t, c, d) index of the partials -> row of the (possibly strided) output
@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* partial, void
   const int c = (int)(row % Hkv);
   const size_t bt = row / Hkv;
   const int t = (int)(bt % N), b = (int)(bt / N);
+  if (t < first_key) return;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     const float* src = partial + (size_t)(which * parts) * elems + i4;
@@ -176,15 +177,15 @@ int launch_sink_combine(const KArgs& a, const Win& win, int dtype, bool small, h
   return small ? launch_sink_combine_t<false, 16, 16>(a, win, st) : launch_sink_combine_t<false, 64, 32>(a, win, st);
 }
 
-int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st) {
+int launch_combine_partials(const KArgs& a, int dtype, hipStream_t st, int first_key) {
   const size_t elems = (size_t)a.B * a.N * a.Hkv * a.D;
   dim3 grid((unsigned)((elems / 4 + 255) / 256));
   if (dtype == S2ATTN_BF16)
     hipLaunchKernelGGL(combine_kernel<true>, grid, dim3(256), 0, st, a.dkv_partial, a.dk, a.dv, a.sdk, a.sdv, a.N,
-                       a.Hkv, a.D, a.parts, elems);
+                       a.Hkv, a.D, a.parts, elems, first_key);
   else
     hipLaunchKernelGGL(combine_kernel<false>, grid, dim3(256), 0, st, a.dkv_partial, a.dk, a.dv, a.sdk, a.sdv, a.N,
-                       a.Hkv, a.D, a.parts, elems);
+                       a.Hkv, a.D, a.parts, elems, first_key);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
