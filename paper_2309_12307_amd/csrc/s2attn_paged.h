@@ -216,11 +216,12 @@ __device__ __forceinline__ int place_of(const PArgs& a, int j0) { return j0 - qu
 __device__ __forceinline__ uint64_t group_off(int page, int at, long long page_bytes, long long token_bytes) {
   return (uint64_t)(uint32_t)page * (uint32_t)page_bytes + (uint32_t)at * (uint32_t)token_bytes;
 }
-// A bit for each of the 16 N keys from j0 on that exists and that some row of the tile sees (is_seen).
+// A bit a key for 16 N keys, and the first n of them.
 template <int N>
 using KeyBits = std::conditional_t<N == 2, uint32_t, uint64_t>;
 template <int N>
 __device__ __forceinline__ KeyBits<N> bits_below(int n) { return n >= 16 * N ? ~KeyBits<N>{0} : n <= 0 ? 0 : (KeyBits<N>{1} << n) - 1; }
+// A bit for each of the 16 N keys from j0 on that exists and that some row of the tile sees (is_seen).
 template <int N>
 __device__ __forceinline__ KeyBits<N> seen_of(const PArgs& a, const Groups<N>& x, int p_lo, int end, int j0) {
   KeyBits<N> seen = 0;

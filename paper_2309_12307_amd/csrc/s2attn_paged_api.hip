@@ -80,10 +80,11 @@ Plan plan(const s2attn_paged_params* p, bool by16) {
   // One token a sequence (as far as T and B tell), of up to 16 rows (e4m3 32 in two blocks, fp32 64 in turns): all go to `few`, by as many
   // tokens as a turn takes: a sequence that has several after all, among empty slots, has workgroups for all of them (256 rows of one
   // of 256 sequences over 8192 keys, H = 64, Hkv = 8, D = 128: 0.60 ms; by turns of one workgroup to a kv head 16.0; as the only
-  // sequence, in `chunk`, 0.09).  Rows that are few in all go there by turns.  Where some sequences have more, those of up to 16 rows (fp32 64) go there and the others to `chunk`.  us, all
-  // in `chunk` and all in `few`, 4000 keys, D = 128: fp32, one sequence of 16 rows 35.8 and 19.9, of 64 65.9 and 57.2, eight of 16 78 and
-  // 56; bf16, one of 16 15.2 and 14.6, of 24 15.6 and 15.9, eight of 20 30.5 and 43.6; e4m3, one of 24 20.4 and 15.4, eight of 20 32 and
-  // 39; one token of 32 sequences, H = 32, bf16 290 and 272, 16 over 30 000 keys, e4m3 558 and 300.
+  // sequence, in `chunk`, 0.09).  Rows that are few in all go there by turns.  Where some sequences have more, those of up to 16
+  // rows (fp32 64) go there and the others to `chunk`.  us, all in `chunk` and all in `few`, 4000 keys, D = 128: fp32, one sequence of 16
+  // rows 35.8 and 19.9, of 64 65.9 and 57.2, eight of 16 78 and 56; bf16, one of 16 15.2 and 14.6, of 24 15.6 and 15.9, eight of 20
+  // 30.5 and 43.6; e4m3, one of 24 20.4 and 15.4, eight of 20 32 and 39; one token of 32 sequences, H = 32, bf16 290 and 272, 16 over
+  // 30 000 keys, e4m3 558 and 300.
   const bool f32 = p->dtype == S2ATTN_F32, e4m3 = p->cache_dtype == S2ATTN_E4M3;
   const long long most_few = f32 ? 64 : e4m3 ? 32 : 16;
   x.nq = 1;
